@@ -41,6 +41,7 @@ extern "C" {
 typedef struct alg_proj_s *alg_proj_t;
 typedef struct alg_ffn_s *alg_ffn_t;
 typedef struct alg_proj_grad_s *alg_proj_grad_t;
+typedef struct alg_ckpt_s *alg_ckpt_t;
 
 typedef enum {
   ALG_OK = 0,
@@ -64,8 +65,9 @@ typedef enum { ALG_F32 = 0, ALG_BF16 = 1 } alg_dtype_t;
  *          (6^L block GEMMs; 36 for q = 4; arithmetic fraction (3/4)^L with equal groups). */
 typedef enum { ALG_TABLE_QQ = 0, ALG_TABLE_DENSE = 1, ALG_TABLE_CUSTOM = 2, ALG_TABLE_Q2POW = 3 } alg_table_t;
 
-/* Activation applied to (acc + bias) before the store. GELU_ERF is z/2 (1 + erf(z/sqrt 2)). */
-typedef enum { ALG_ACT_NONE = 0, ALG_ACT_GELU_ERF = 1, ALG_ACT_GELU_TANH = 2 } alg_act_t;
+/* Activation applied to (acc + bias) before the store. GELU_ERF is z/2 (1 + erf(z/sqrt 2)).
+ * SILU, z / (1 + exp(-z)), is an activation of the alg_ckpt_* calls only (the gated FFN has it built in). */
+typedef enum { ALG_ACT_NONE = 0, ALG_ACT_GELU_ERF = 1, ALG_ACT_GELU_TANH = 2, ALG_ACT_SILU = 3 } alg_act_t;
 
 /* EXPLICIT: the caller passes types[M] with every forward call.
  * CYCLIC  : type of row b is b mod q (the paper's example schedule tau(p) = p mod q for a
@@ -360,6 +362,39 @@ alg_status_t alg_proj_grad_weight(alg_proj_grad_t h, const void *X, int64_t ldx,
                                   int64_t lddw, alg_dtype_t w_dtype, void *workspace,
                                   size_t workspace_bytes, void *stream);
 alg_status_t alg_proj_grad_last_status(alg_proj_grad_t h, void *stream, alg_status_t *status);
+
+/* ---- activations kept in 8 bits between the two passes of a training step ------------------------------
+ * The gradient maps above need X and the gradient of every projection; the activation between the up and the
+ * down projection needs its own input.  A checkpoint handle keeps such matrices at 8 bits a value: M records of
+ * alg_ckpt_row_bytes bytes, one for each row, that hold
+ *     codes   part 0 (and part 1 of a gated handle): `cols` codes, padded to a multiple of 32 with zero codes
+ *     scales  one byte s for each 32 codes, in the codes' order: a code c stands for c * 2^(s - 127)
+ * with the rest of the record unspecified.  The scale of a block is the smallest power of two under which its
+ * largest magnitude fits the format (448 for E4M3, 127 for INT8), at least 2^-120, so the codes are exact functions of the
+ * values: a value is off by at most 2^-4 of itself (E4M3, above the format's subnormals) or half a step of its
+ * block (INT8).  A block that holds an infinity or a NaN has s = 255 and reads back as NaN.
+ *   store / load     X (M x cols, x_dtype, ungated handles) to records and back
+ *   act_forward      A = act(Z), ungated, Z M x cols; or A = act(G) .* U with Z = [G | U] M x 2 cols, gated.  Writes the
+ *                    record of Z beside A in the same pass; ckpt == NULL keeps nothing.
+ *   act_backward     from the records of Z (as they read back) and dA (M x cols): dZ = act'(Z) .* dA, or
+ *                    [act'(G) .* U .* dA | act(G) .* dA]; with A not NULL also the activation once more, for
+ *                    the weight gradient of the down projection.
+ * One dtype a call: Z, A, dA and dZ are all f32 or all bf16 (arithmetic in fp32, rounded once).  Leading dimensions and
+ * addresses may be anything an element may have; rows on 16 bytes with cols a multiple of 8 run several
+ * times faster.  ckpt: 16-byte aligned.  A may be Z and dZ may be dA where both have the same shape and leading dimension;
+ * any other overlap of outputs with operands is ALG_ERR_INVALID_ARG.  M = 0 is a successful no-op.  One launch a call,
+ * no workspace; the calls keep nothing in the handle, so they may overlap on any streams. */
+typedef enum { ALG_Q8_E4M3 = 0, ALG_Q8_INT8 = 1 } alg_q8_t;
+#define ALG_CKPT_MAX_COLS 262144
+alg_status_t alg_ckpt_create(alg_ckpt_t *out, int cols, alg_q8_t format, alg_act_t act, int gated);
+alg_status_t alg_ckpt_destroy(alg_ckpt_t h);
+alg_status_t alg_ckpt_row_bytes(alg_ckpt_t h, size_t *bytes);
+alg_status_t alg_ckpt_store(alg_ckpt_t h, const void *X, int64_t ldx, alg_dtype_t x_dtype, int64_t M, void *ckpt, void *stream);
+alg_status_t alg_ckpt_load(alg_ckpt_t h, const void *ckpt, int64_t M, void *X, int64_t ldx, alg_dtype_t x_dtype, void *stream);
+alg_status_t alg_ckpt_act_forward(alg_ckpt_t h, const void *Z, int64_t ldz, int64_t M, void *A, int64_t lda, alg_dtype_t dtype,
+                                  void *ckpt, void *stream);
+alg_status_t alg_ckpt_act_backward(alg_ckpt_t h, const void *ckpt, const void *dA, int64_t ldda, int64_t M, void *dZ, int64_t lddz,
+                                   void *A, int64_t lda, alg_dtype_t dtype, void *stream);
 
 /* alg_proj_forward with X, types and Y in HOST memory (packed rows: ldx = K, ldy = N; pinned
  * memory makes the copies asynchronous): copies X and types to device staging inside the

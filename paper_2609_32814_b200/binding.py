@@ -19,8 +19,9 @@ STATUS = {0: "ALG_OK", 1: "ALG_ERR_INVALID_ARG", 2: "ALG_ERR_UNSUPPORTED_SHAPE",
           4: "ALG_ERR_CUDA", 5: "ALG_ERR_BAD_TYPE", 6: "ALG_ERR_DEVICE_TIMEOUT"}
 ALG_F32, ALG_BF16 = 0, 1
 ALG_TABLE_QQ, ALG_TABLE_DENSE, ALG_TABLE_CUSTOM, ALG_TABLE_Q2POW = 0, 1, 2, 3
-ALG_ACT_NONE, ALG_ACT_GELU_ERF, ALG_ACT_GELU_TANH = 0, 1, 2
+ALG_ACT_NONE, ALG_ACT_GELU_ERF, ALG_ACT_GELU_TANH, ALG_ACT_SILU = 0, 1, 2, 3
 ALG_SCHED_EXPLICIT, ALG_SCHED_CYCLIC, ALG_SCHED_INTERVAL = 0, 1, 2
+ALG_Q8_E4M3, ALG_Q8_INT8 = 0, 1
 ALG_PATH_SIMT, ALG_PATH_TCGEN05, ALG_PATH_DECODE = 0, 1, 2
 OPTIONS = {"gemm_kernel": 1, "tile_n": 2, "small_m_kernel": 3, "host_plan": 4, "wait_limit_cycles": 5,
            "test_stall_bytes": 6, "stage_k": 7, "interval_period": 8, "row_gather": 9, "weight_packed": 10}
@@ -29,6 +30,8 @@ _DTYPES = {"f32": ALG_F32, "bf16": ALG_BF16, torch.float32: ALG_F32, torch.bfloa
 _TABLES = {"qq": ALG_TABLE_QQ, "dense": ALG_TABLE_DENSE, "custom": ALG_TABLE_CUSTOM, "q2pow": ALG_TABLE_Q2POW}
 _ACTS = {None: ALG_ACT_NONE, "none": ALG_ACT_NONE, "gelu": ALG_ACT_GELU_ERF, "gelu_erf": ALG_ACT_GELU_ERF,
          "gelu_tanh": ALG_ACT_GELU_TANH}
+_CKPT_ACTS = {**_ACTS, "silu": ALG_ACT_SILU}
+_Q8 = {"e4m3": ALG_Q8_E4M3, "int8": ALG_Q8_INT8}
 _SCHEDS = {"explicit": ALG_SCHED_EXPLICIT, "cyclic": ALG_SCHED_CYCLIC, "interval": ALG_SCHED_INTERVAL}
 
 EXPORTS = [
@@ -37,6 +40,8 @@ EXPORTS = [
     "alg_ffn_workspace_bytes", "alg_ffn_forward", "alg_ffn_host_workspace_bytes", "alg_ffn_forward_host",
     "alg_ffn_gated_create", "alg_ffn_gated_forward", "alg_proj_grad_create", "alg_proj_grad_destroy",
     "alg_proj_grad_workspace_bytes", "alg_proj_grad_input", "alg_proj_grad_weight", "alg_proj_grad_last_status", "alg_ffn_macs", "alg_ffn_last_status", "alg_ffn_set_timing", "alg_ffn_get_timing", "alg_status_string", "alg_launch_count",
+    "alg_ckpt_create", "alg_ckpt_destroy", "alg_ckpt_row_bytes", "alg_ckpt_store", "alg_ckpt_load", "alg_ckpt_act_forward",
+    "alg_ckpt_act_backward",
 ]
 
 _lib = None
@@ -91,6 +96,13 @@ def lib() -> ctypes.CDLL:
         L.alg_ffn_last_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         L.alg_ffn_set_timing.argtypes = [vp, i32]
         L.alg_ffn_get_timing.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
+        L.alg_ckpt_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, i32]
+        L.alg_ckpt_destroy.argtypes = [vp]
+        L.alg_ckpt_row_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
+        L.alg_ckpt_store.argtypes = [vp, vp, i64, i32, i64, vp, vp]
+        L.alg_ckpt_load.argtypes = [vp, vp, i64, vp, i64, i32, vp]
+        L.alg_ckpt_act_forward.argtypes = [vp, vp, i64, i64, vp, i64, i32, vp, vp]
+        L.alg_ckpt_act_backward.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp, i64, i32, vp]
         L.alg_status_string.argtypes = [i32]
         L.alg_status_string.restype = ctypes.c_char_p
         L.alg_launch_count.argtypes = []
@@ -114,6 +126,20 @@ def _stream(stream=None):
         return stream.cuda_stream
     # what torch.cuda.current_stream().cuda_stream is, without the Stream object (3.3 -> 0.3 us)
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _rows(t, what, M, cols, dtype, device):
+    """The leading dimension of an M x cols operand with contiguous rows, of this dtype, on the handle's device."""
+    if t.dim() != 2 or t.shape[0] != M or t.shape[1] != cols:
+        raise ValueError(f"{what} must be {M} x {cols}, got {tuple(t.shape)}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{what} must be on the handle's device, cuda:{device}")
+    ld, step = t.stride()
+    if (step != 1 and cols > 1) or (ld < cols and M > 1):
+        raise ValueError(f"{what} must have contiguous rows that do not overlap")
+    return ld if M > 1 else cols
 
 
 def _widths(w):
@@ -408,3 +434,74 @@ class ProjGrad(_Handle):
         s = ctypes.c_int()
         _check(lib().alg_proj_grad_last_status(self._h, _stream(stream), ctypes.byref(s)), "alg_proj_grad_last_status")
         return s.value
+
+
+class ActCheckpoint(_Handle):
+    """alg_ckpt_* : an activation's input, or any other matrix, kept in 8 bits for the backward pass.
+
+    ``cols`` is the width of A = act(Z), or of X for store and load; a gated handle takes Z = [G | U], 2 cols wide.  A
+    checkpoint is a uint8 tensor of M records (``new``), whose rows can be sliced."""
+    _destroy = "alg_ckpt_destroy"
+
+    def __init__(self, cols, act=None, gated=False, fmt="e4m3"):
+        super().__init__()
+        self.cols, self.wide = int(cols), int(cols) * (2 if gated else 1)
+        _check(lib().alg_ckpt_create(ctypes.byref(self._h), self.cols, _Q8[fmt], _CKPT_ACTS[act], int(bool(gated))), "alg_ckpt_create")
+        self._device = torch.cuda.current_device()
+        out = ctypes.c_size_t()
+        _check(lib().alg_ckpt_row_bytes(self._h, ctypes.byref(out)), "alg_ckpt_row_bytes")
+        self.row_bytes = out.value
+
+    def set_option(self, name, value):
+        raise NotImplementedError("checkpoint handles have no options")
+
+    def new(self, M):
+        """Memory for M records."""
+        return torch.empty((M, self.row_bytes), dtype=torch.uint8, device=f"cuda:{self._device}")
+
+    def _records(self, ckpt, M):
+        if _rows(ckpt, "the checkpoint", M, self.row_bytes, torch.uint8, self._device) != self.row_bytes:
+            raise ValueError("the checkpoint's records must be packed")
+        return ckpt.data_ptr()
+
+    def _out(self, out, what, M, cols, dtype):
+        if out is None:
+            out = torch.empty((M, cols), dtype=dtype, device=f"cuda:{self._device}")
+            return out, cols
+        return out, _rows(out, what, M, cols, dtype, self._device)
+
+    def store(self, X, out=None, stream=None):
+        """The checkpoint of X."""
+        M = X.shape[0]
+        ldx = _rows(X, "X", M, self.cols, X.dtype, self._device)
+        out = self.new(M) if out is None else out
+        _check(lib().alg_ckpt_store(self._h, X.data_ptr(), ldx, _DTYPES[X.dtype], M, self._records(out, M), _stream(stream)), "alg_ckpt_store")
+        return out
+
+    def load(self, ckpt, out=None, out_dtype=torch.bfloat16, stream=None):
+        """The values a checkpoint stands for."""
+        M = ckpt.shape[0]
+        out, ldo = self._out(out, "out", M, self.cols, out_dtype if out is None else out.dtype)
+        _check(lib().alg_ckpt_load(self._h, self._records(ckpt, M), M, out.data_ptr(), ldo, _DTYPES[out.dtype], _stream(stream)), "alg_ckpt_load")
+        return out
+
+    def forward(self, Z, out=None, ckpt=None, keep=True, stream=None):
+        """(A, checkpoint of Z); keep=False: (A, None), nothing is kept."""
+        M = Z.shape[0]
+        ldz = _rows(Z, "Z", M, self.wide, Z.dtype, self._device)
+        out, ldo = self._out(out, "out", M, self.cols, Z.dtype)
+        if keep and ckpt is None:
+            ckpt = self.new(M)
+        _check(lib().alg_ckpt_act_forward(self._h, Z.data_ptr(), ldz, M, out.data_ptr(), ldo, _DTYPES[Z.dtype],
+                                          self._records(ckpt, M) if keep else None, _stream(stream)), "alg_ckpt_act_forward")
+        return out, ckpt if keep else None
+
+    def backward(self, ckpt, dA, out=None, again=True, stream=None):
+        """(dZ, A) from the checkpoint of Z and the gradient of A.  ``again``: a tensor for A, True for a new one, False for none."""
+        M = dA.shape[0]
+        ldd = _rows(dA, "dA", M, self.cols, dA.dtype, self._device)
+        out, ldo = self._out(out, "out", M, self.wide, dA.dtype)
+        A, lda = (None, 0) if again is False or again is None else self._out(None if again is True else again, "again", M, self.cols, dA.dtype)
+        _check(lib().alg_ckpt_act_backward(self._h, self._records(ckpt, M), dA.data_ptr(), ldd, M, out.data_ptr(), ldo, _ptr(A), lda,
+                                           _DTYPES[dA.dtype], _stream(stream)), "alg_ckpt_act_backward")
+        return out, A

@@ -1,0 +1,94 @@
+// What the row-wise kernels around the projections share: eight consecutive values of a row in either type, and the
+// host's checks of their operands.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "algproj.h"
+
+namespace algproj {
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void from_f32(float v, float *dst) { *dst = v; }
+__device__ __forceinline__ void from_f32(float v, __nv_bfloat16 *dst) { *dst = __float2bfloat16_rn(v); }
+
+// Eight consecutive values as they lie in memory: 16 bytes of bf16, 32 of fp32.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = *(const uint4 *)p; }
+  __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void set(int j, __nv_bfloat16 v) { ((__nv_bfloat16 *)&a)[j] = v; }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[2 * j] = __uint_as_float(w[j] << 16), f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+  }
+};
+template <>
+struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void set(int j, float v) { (j < 4 ? (float *)&a : (float *)&b)[j & 3] = v; }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  }
+};
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&f)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+    w[j] = *(const uint32_t *)&v;
+  }
+  *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(float *p, const float (&f)[8]) {
+  ((float4 *)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+  ((float4 *)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+
+inline size_t elem_size(alg_dtype_t t) { return t == ALG_BF16 ? 2 : 4; }
+inline bool on_16(const void *p, int64_t ld, size_t elem) { return ((uintptr_t)p & 15u) == 0 && ((size_t)ld * elem) % 16 == 0; }
+inline bool on_element(const void *p, size_t elem) { return (uintptr_t)p % elem == 0; }
+
+// M rows of `width` bytes, `pitch` bytes apart.
+struct RowSpan {
+  uintptr_t at;
+  size_t pitch, width;
+  int64_t rows;
+  uintptr_t end() const { return at + (size_t)(rows - 1) * pitch + width; }
+};
+inline RowSpan span(const void *p, int64_t ld, int64_t cols, size_t elem, int64_t M) {
+  return {(uintptr_t)p, (size_t)ld * elem, (size_t)cols * elem, M};
+}
+// Whether two matrices may share a byte (column slices of one buffer do not).
+inline bool meet(const RowSpan &a, const RowSpan &b) {
+  if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0 || a.end() <= b.at || b.end() <= a.at) return false;
+  if (a.pitch != b.pitch) return true;
+  const RowSpan &lo = a.at <= b.at ? a : b, &hi = a.at <= b.at ? b : a;
+  const size_t d = (hi.at - lo.at) % a.pitch;
+  return d < lo.width || d + hi.width > a.pitch;
+}
+inline bool same_rows(const RowSpan &a, const RowSpan &b) { return a.at == b.at && a.pitch == b.pitch && a.width == b.width; }
+
+// The current device, which has to be the one a handle was made on, and of the kind the kernels are built for.
+inline alg_status_t kernel_device(int *dev, int *num_sms) {
+  int major = 0;
+  if (cudaGetDevice(dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(num_sms, cudaDevAttrMultiProcessorCount, *dev) != cudaSuccess)
+    return ALG_ERR_CUDA;
+  return major == 10 ? ALG_OK : ALG_ERR_UNSUPPORTED_SHAPE;
+}
+inline bool is_current(int device) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == device;
+}
+
+}  // namespace algproj
