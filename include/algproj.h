@@ -41,6 +41,7 @@ extern "C" {
 typedef struct alg_proj_s *alg_proj_t;
 typedef struct alg_ffn_s *alg_ffn_t;
 typedef struct alg_proj_grad_s *alg_proj_grad_t;
+typedef struct alg_norm_s *alg_norm_t;
 typedef struct alg_ckpt_s *alg_ckpt_t;
 
 typedef enum {
@@ -362,6 +363,55 @@ alg_status_t alg_proj_grad_weight(alg_proj_grad_t h, const void *X, int64_t ldx,
                                   int64_t lddw, alg_dtype_t w_dtype, void *workspace,
                                   size_t workspace_bytes, void *stream);
 alg_status_t alg_proj_grad_last_status(alg_proj_grad_t h, void *stream, alg_status_t *status);
+
+/* ---- a block's border: norms before and after a block, with its gate and residual scale ----------------
+ * With the block's output F and the residual stream R (both M x D), in one pass:
+ *     V = norm(F)                          (flag POST; else V = F)
+ *     Y = R + alpha * scale .* g .* (V .* post_weight + post_bias)
+ *     N = norm(Y) .* pre_weight + pre_bias (flag PRE: the input of the next block)
+ * norm is RMS (x / sqrt(mean x^2 + eps)) or LAYER ((x - mean) / sqrt(var + eps)), over the D features of a row.  The gate g is
+ * one value for each row (GATE_ROW, gate[M]) or each element (GATE_ELEMENT, M x D), taken as it is or through a
+ * sigmoid (GATE_SIGMOID); 1 without a gate flag.  A handle without JOIN has no F: Y is R, and only N is written (a plain norm).
+ * R, Y and their gradients have stream_dtype, F, gate, N and theirs dtype (f32 or bf16 each); statistics, sums and all arithmetic
+ * are fp32, and N is normed from Y before Y is rounded.  The vectors (post_weight, post_bias, scale, pre_weight, pre_bias: D fp32 values)
+ * may each be NULL: weights and scale of 1, biases of 0.
+ *   backward   from Y as the forward pass stored it (R without JOIN), F, gate and the gradients dY (NULL: zero) and dN (PRE handles):
+ *                  dR = dY + the gradient through N;     with T = alpha * dR:
+ *                  dF = gradient through V of  T .* scale .* g .* post_weight,
+ *                  dgate = T .* scale .* (V .* post_weight + post_bias) (times the sigmoid's slope; summed over a row for GATE_ROW),
+ *              and the column sums d_post_weight, d_post_bias, d_scale, d_pre_weight, d_pre_bias (D fp32 values each, overwritten; NULL:
+ *              not wanted; the biases' need no biases in the forward pass).  dF needs JOIN, dgate a gate flag, d_post_* POST, d_pre_*
+ *              PRE, d_scale JOIN; dF and dgate may be NULL.  Sums run in a fixed order: bitwise repeatable.
+ * 1 <= D <= ALG_NORM_MAX_D.  Leading dimensions and addresses may be anything an element may have; D a multiple of 8 with all
+ * rows on 16 bytes (vectors too) runs several times faster.  Row b of an output may lie exactly on row b of an operand (Y on R, dR on
+ * dY, ...: same address, leading dimension and row length in bytes); any other overlap is ALG_ERR_INVALID_ARG.  M = 0: forward
+ * is a no-op, backward writes zero sums.  Workspace (backward): alg_norm_workspace_bytes, 256-byte aligned, no
+ * initialisation needed; calls that share one must be ordered on the GPU, others may overlap on any streams.  Forward is one launch,
+ * backward two (one without column sums). */
+typedef enum { ALG_NORM_RMS = 0, ALG_NORM_LAYER = 1 } alg_norm_kind_t;
+#define ALG_NORM_JOIN 1
+#define ALG_NORM_PRE 2
+#define ALG_NORM_POST 4
+#define ALG_NORM_GATE_ROW 8
+#define ALG_NORM_GATE_ELEMENT 16
+#define ALG_NORM_GATE_SIGMOID 32
+#define ALG_NORM_MAX_D 8192
+alg_status_t alg_norm_create(alg_norm_t *out, int D, alg_norm_kind_t kind, int flags, float eps, alg_dtype_t stream_dtype,
+                             alg_dtype_t dtype);
+alg_status_t alg_norm_destroy(alg_norm_t h);
+alg_status_t alg_norm_workspace_bytes(alg_norm_t h, size_t *bytes);
+alg_status_t alg_norm_forward(alg_norm_t h, const void *R, int64_t ldr, const void *F, int64_t ldf, const void *gate, int64_t ldg,
+                              const float *post_weight, const float *post_bias, const float *scale, float alpha,
+                              const float *pre_weight, const float *pre_bias, int64_t M, void *Y, int64_t ldy, void *N, int64_t ldn,
+                              void *stream);
+alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const void *dY, int64_t lddy, const void *dN, int64_t lddn,
+                               const void *F, int64_t ldf, const void *gate, int64_t ldg, const float *post_weight,
+                               const float *post_bias, const float *scale, float alpha, const float *pre_weight, int64_t M, void *dR,
+                               int64_t lddr, void *dF, int64_t lddf, void *dgate, int64_t lddg, float *d_post_weight,
+                               float *d_post_bias, float *d_scale, float *d_pre_weight, float *d_pre_bias, void *workspace,
+                               size_t workspace_bytes, void *stream);
+/* Reads and clears the handle's device status word, as alg_proj_last_status. */
+alg_status_t alg_norm_last_status(alg_norm_t h, void *stream, alg_status_t *status);
 
 /* ---- activations kept in 8 bits between the two passes of a training step ------------------------------
  * The gradient maps above need X and the gradient of every projection; the activation between the up and the

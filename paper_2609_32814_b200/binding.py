@@ -22,6 +22,8 @@ ALG_TABLE_QQ, ALG_TABLE_DENSE, ALG_TABLE_CUSTOM, ALG_TABLE_Q2POW = 0, 1, 2, 3
 ALG_ACT_NONE, ALG_ACT_GELU_ERF, ALG_ACT_GELU_TANH, ALG_ACT_SILU = 0, 1, 2, 3
 ALG_SCHED_EXPLICIT, ALG_SCHED_CYCLIC, ALG_SCHED_INTERVAL = 0, 1, 2
 ALG_Q8_E4M3, ALG_Q8_INT8 = 0, 1
+ALG_NORM_RMS, ALG_NORM_LAYER = 0, 1
+ALG_NORM_JOIN, ALG_NORM_PRE, ALG_NORM_POST, ALG_NORM_GATE_ROW, ALG_NORM_GATE_ELEMENT, ALG_NORM_GATE_SIGMOID = 1, 2, 4, 8, 16, 32
 ALG_PATH_SIMT, ALG_PATH_TCGEN05, ALG_PATH_DECODE = 0, 1, 2
 OPTIONS = {"gemm_kernel": 1, "tile_n": 2, "small_m_kernel": 3, "host_plan": 4, "wait_limit_cycles": 5,
            "test_stall_bytes": 6, "stage_k": 7, "interval_period": 8, "row_gather": 9, "weight_packed": 10}
@@ -40,6 +42,7 @@ EXPORTS = [
     "alg_ffn_workspace_bytes", "alg_ffn_forward", "alg_ffn_host_workspace_bytes", "alg_ffn_forward_host",
     "alg_ffn_gated_create", "alg_ffn_gated_forward", "alg_proj_grad_create", "alg_proj_grad_destroy",
     "alg_proj_grad_workspace_bytes", "alg_proj_grad_input", "alg_proj_grad_weight", "alg_proj_grad_last_status", "alg_ffn_macs", "alg_ffn_last_status", "alg_ffn_set_timing", "alg_ffn_get_timing", "alg_status_string", "alg_launch_count",
+    "alg_norm_create", "alg_norm_destroy", "alg_norm_workspace_bytes", "alg_norm_forward", "alg_norm_backward", "alg_norm_last_status",
     "alg_ckpt_create", "alg_ckpt_destroy", "alg_ckpt_row_bytes", "alg_ckpt_store", "alg_ckpt_load", "alg_ckpt_act_forward",
     "alg_ckpt_act_backward",
 ]
@@ -96,6 +99,13 @@ def lib() -> ctypes.CDLL:
         L.alg_ffn_last_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         L.alg_ffn_set_timing.argtypes = [vp, i32]
         L.alg_ffn_get_timing.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
+        L.alg_norm_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, ctypes.c_float, i32, i32]
+        L.alg_norm_destroy.argtypes = [vp]
+        L.alg_norm_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
+        L.alg_norm_forward.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, ctypes.c_float, vp, vp, i64, vp, i64, vp, i64, vp]
+        L.alg_norm_backward.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, ctypes.c_float, vp, i64, vp, i64, vp, i64,
+                                        vp, i64, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.alg_norm_last_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         L.alg_ckpt_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, i32]
         L.alg_ckpt_destroy.argtypes = [vp]
         L.alg_ckpt_row_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
@@ -433,6 +443,112 @@ class ProjGrad(_Handle):
     def last_status(self, stream=None) -> int:
         s = ctypes.c_int()
         _check(lib().alg_proj_grad_last_status(self._h, _stream(stream), ctypes.byref(s)), "alg_proj_grad_last_status")
+        return s.value
+
+
+class BlockNorm(_Handle):
+    """alg_norm_* : Y = R + alpha * scale * gate * (norm(F) * post_weight + post_bias),  N = norm(Y) * pre_weight + pre_bias.
+
+    ``join``: F is added to the residual stream R (else Y is R); ``post``: F is normed; ``pre``: N is wanted; ``gate``: None, "row"
+    (one value for each row) or "element".  R, Y and their gradients have ``stream_dtype``, F, gate, N and theirs ``dtype``."""
+    _destroy = "alg_norm_destroy"
+
+    def __init__(self, D, kind="rms", join=False, pre=True, post=False, gate=None, gate_act=None, eps=1e-6, dtype="bf16", stream_dtype="bf16"):
+        super().__init__()
+        self.D, self.join, self.pre, self.post, self.gate = int(D), bool(join), bool(pre), bool(post), gate
+        self.stream_type, self.type = (torch.float32 if _DTYPES[t] == ALG_F32 else torch.bfloat16 for t in (stream_dtype, dtype))
+        flags = ((ALG_NORM_JOIN if join else 0) | (ALG_NORM_PRE if pre else 0) | (ALG_NORM_POST if post else 0) |
+                 {None: 0, "row": ALG_NORM_GATE_ROW, "element": ALG_NORM_GATE_ELEMENT}[gate] |
+                 {None: 0, "sigmoid": ALG_NORM_GATE_SIGMOID}[gate_act])
+        _check(lib().alg_norm_create(ctypes.byref(self._h), self.D, {"rms": ALG_NORM_RMS, "layer": ALG_NORM_LAYER}[kind], flags, float(eps),
+                                     _DTYPES[stream_dtype], _DTYPES[dtype]), "alg_norm_create")
+        self._device = torch.cuda.current_device()
+        out = ctypes.c_size_t()
+        _check(lib().alg_norm_workspace_bytes(self._h, ctypes.byref(out)), "alg_norm_workspace_bytes")
+        self._bytes = out.value
+
+    def set_option(self, name, value):
+        raise NotImplementedError("norm handles have no options")
+
+    def workspace_bytes(self) -> int:
+        """Bytes a backward call with column sums needs."""
+        return self._bytes
+
+    def _matrix(self, t, what, M, dtype):
+        """(address, leading dimension) of an operand."""
+        if t is None:
+            return None, 0
+        return t.data_ptr(), _rows(t, what, M, self.D, dtype, self._device)
+
+    def _gate(self, t, what, M):
+        if t is None or self.gate != "row":
+            return self._matrix(t, what, M, self.type)
+        if t.shape != (M,) or t.dtype is not self.type or t.get_device() != self._device or (M > 1 and t.stride(0) != 1):
+            raise ValueError(f"{what} must hold {M} packed {self.type} values on the handle's device")
+        return t.data_ptr(), 0
+
+    def _vector(self, t, what):
+        if t is None:
+            return None
+        if t.shape != (self.D,) or t.dtype is not torch.float32 or t.get_device() != self._device or (self.D > 1 and t.stride(0) != 1):
+            raise ValueError(f"{what} must hold {self.D} packed float32 values on the handle's device")
+        return t.data_ptr()
+
+    def _new(self, M, dtype):
+        return torch.empty((M, self.D), dtype=dtype, device=f"cuda:{self._device}")
+
+    def forward(self, R, F=None, gate=None, post_weight=None, post_bias=None, scale=None, alpha=1.0, pre_weight=None, pre_bias=None, out=None,
+                normed=None, stream=None):
+        """(Y, N); Y is R without ``join``, N is None without ``pre``."""
+        M = R.shape[0]
+        if self.join and out is None:
+            out = self._new(M, self.stream_type)
+        if self.pre and normed is None:
+            normed = self._new(M, self.type)
+        _check(lib().alg_norm_forward(self._h, *self._matrix(R, "R", M, self.stream_type), *self._matrix(F, "F", M, self.type),
+                                      *self._gate(gate, "gate", M), self._vector(post_weight, "post_weight"), self._vector(post_bias, "post_bias"),
+                                      self._vector(scale, "scale"), alpha, self._vector(pre_weight, "pre_weight"),
+                                      self._vector(pre_bias, "pre_bias"), M, *self._matrix(out, "out", M, self.stream_type),
+                                      *self._matrix(normed, "normed", M, self.type), _stream(stream)), "alg_norm_forward")
+        return (out if self.join else R), normed
+
+    def backward(self, Y, dY=None, dN=None, F=None, gate=None, post_weight=None, post_bias=None, scale=None, alpha=1.0, pre_weight=None,
+                 pre_bias=None, want=None, out=None, workspace=None, stream=None):
+        """The gradients, by name: "R", "F", "gate" and those of the vectors given.  ``want``: the names to compute (R always is) instead of
+        all of these; ``out``: tensors to write some of them to."""
+        M = Y.shape[0]
+        given = {"post_weight": post_weight, "post_bias": post_bias, "scale": scale, "pre_weight": pre_weight, "pre_bias": pre_bias}
+        if want is None:
+            want = [k for k, v in given.items() if v is not None] + ["F", "gate"][:(1 + (self.gate is not None)) if self.join else 0]
+        got = dict(out) if out else {}
+        for k in ("R", *want):
+            if k in got:
+                continue
+            if k in given:
+                got[k] = torch.empty((self.D,), dtype=torch.float32, device=f"cuda:{self._device}")
+            elif k == "gate" and self.gate == "row":
+                got[k] = torch.empty((M,), dtype=self.type, device=f"cuda:{self._device}")
+            elif k in ("R", "F", "gate"):
+                got[k] = self._new(M, self.stream_type if k == "R" else self.type)
+            else:
+                raise ValueError(f"no gradient is called {k}")
+        ws = None
+        if any(k in got for k in given):
+            ws = workspace if workspace is not None else self._workspace(self._bytes, Y.device)
+        vec = [self._vector(got.get(k), f"the gradient of {k}") for k in given]
+        _check(lib().alg_norm_backward(self._h, *self._matrix(Y, "Y", M, self.stream_type), *self._matrix(dY, "dY", M, self.stream_type),
+                                       *self._matrix(dN, "dN", M, self.type), *self._matrix(F, "F", M, self.type), *self._gate(gate, "gate", M),
+                                       self._vector(post_weight, "post_weight"), self._vector(post_bias, "post_bias"),
+                                       self._vector(scale, "scale"), alpha, self._vector(pre_weight, "pre_weight"), M,
+                                       *self._matrix(got["R"], "the gradient of R", M, self.stream_type),
+                                       *self._matrix(got.get("F"), "the gradient of F", M, self.type),
+                                       *self._gate(got.get("gate"), "the gradient of gate", M), *vec, _ptr(ws), 0 if ws is None else ws.numel(),
+                                       _stream(stream)), "alg_norm_backward")
+        return got
+
+    def last_status(self, stream=None) -> int:
+        s = ctypes.c_int()
+        _check(lib().alg_norm_last_status(self._h, _stream(stream), ctypes.byref(s)), "alg_norm_last_status")
         return s.value
 
 

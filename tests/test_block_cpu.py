@@ -21,3 +21,24 @@ def test_checkpoint_handles_refuse_bad_arguments_first():
     assert L.alg_ckpt_store(None, None, 0, 0, 0, None, None) == 1 and L.alg_ckpt_load(None, None, 0, None, 0, 0, None) == 1
     assert L.alg_ckpt_act_forward(None, None, 0, 0, None, 0, 0, None, None) == 1
     assert L.alg_ckpt_act_backward(None, None, None, 0, 0, None, 0, None, 0, 0, None) == 1
+
+
+def test_norm_handles_refuse_bad_arguments_first():
+    L, h = _lib(), ctypes.c_void_p()
+    ref = ctypes.byref(h)
+    nan, inf = float("nan"), float("inf")
+    assert L.alg_norm_create(None, 64, 0, 2, 1e-6, 1, 1) == 1
+    for D, kind, flags, eps, st, dt in ((0, 0, 2, 1e-6, 1, 1), (64, 2, 2, 1e-6, 1, 1), (64, 0, 0, 1e-6, 1, 1), (64, 0, 4, 1e-6, 1, 1),
+                                        (64, 0, 2 | 4, 1e-6, 1, 1), (64, 0, 1 | 8 | 16, 1e-6, 1, 1), (64, 0, 1 | 32, 1e-6, 1, 1),
+                                        (64, 0, 64 | 2, 1e-6, 1, 1), (64, 0, -1, 1e-6, 1, 1), (64, 0, 2, -1e-6, 1, 1), (64, 0, 2, nan, 1, 1),
+                                        (64, 0, 2, inf, 1, 1), (64, 0, 2, 1e-6, 2, 1), (64, 0, 2, 1e-6, 1, -1)):
+        assert L.alg_norm_create(ref, D, kind, flags, eps, st, dt) == 1
+        assert not h.value
+    assert L.alg_norm_create(ref, 8193, 0, 2, 1e-6, 1, 1) == 2
+    n = ctypes.c_size_t()
+    assert L.alg_norm_workspace_bytes(None, ctypes.byref(n)) == 1 and L.alg_norm_destroy(None) == 1
+    assert L.alg_norm_forward(None, None, 0, None, 0, None, 0, None, None, None, 1.0, None, None, 0, None, 0, None, 0, None) == 1
+    assert L.alg_norm_backward(None, None, 0, None, 0, None, 0, None, 0, None, 0, None, None, None, 1.0, None, 0, None, 0, None, 0, None, 0, None,
+                               None, None, None, None, None, 0, None) == 1
+    s = ctypes.c_int()
+    assert L.alg_norm_last_status(None, None, ctypes.byref(s)) == 1

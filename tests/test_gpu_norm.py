@@ -1,0 +1,341 @@
+"""The border of a block -- norms before and after it, gate, residual scale -- and its gradients, against the definitions in 64 bits
+(gradients by autograd of the definition).
+
+Tolerances.  All arithmetic is fp32 with sums of at most 16 columns a thread, then trees: 16 + 10 additions, a reciprocal root of 2 units,
+sigmoids of 4 units and fewer than 20 roundings otherwise, so every result is off by at most 64 * 2^-24 of the sum of the magnitudes that went
+into it (written beside each), plus half a step of its type.  Column sums add at most 14 rows a thread, 15 groups, 19 CTAs and 8 slices: the
+same 64 once more."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_32814_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+EPS = 1e-5
+U = 64 * 2.0 ** -24
+
+
+def norm(x, kind, w=None, b=None):
+    mu = x.mean(1, keepdim=True) if kind == "layer" else 0.0
+    v = (x - mu) / torch.sqrt(((x - mu) ** 2).mean(1, keepdim=True) + EPS)
+    v = v if w is None else v * w
+    return v if b is None else v + b
+
+
+def norm_size(x, kind, w=None, b=None):
+    """Magnitudes behind norm(x)."""
+    r = 1 / torch.sqrt(((x - (x.mean(1, keepdim=True) if kind == "layer" else 0.0)) ** 2).mean(1, keepdim=True) + EPS)
+    v = (x.abs() + (x.abs().mean(1, keepdim=True) if kind == "layer" else 0.0)) * r
+    v = v if w is None else v * w.abs()
+    return v if b is None else v + b.abs()
+
+
+def through(x, kind, h):
+    """Magnitudes behind the gradient of the normed x for the gradient h."""
+    mu = x.mean(1, keepdim=True) if kind == "layer" else 0.0
+    r = 1 / torch.sqrt(((x - mu) ** 2).mean(1, keepdim=True) + EPS)
+    v = (x.abs() + (x.abs().mean(1, keepdim=True) if kind == "layer" else 0.0)) * r
+    h = h.abs()
+    return 2 * r * (h + h.mean(1, keepdim=True) + v * (h * v).mean(1, keepdim=True))
+
+
+def near(got, want, size, what, u=U):
+    assert got.shape == want.shape, what
+    bound = u * size + torch.finfo(got.dtype).eps / 2 * want.abs() + 1e-30
+    off = (got.double().cpu() - want).abs()
+    bad = ~(off <= bound)
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()}, worst {float((off / bound).max()):.2f} of the bound"
+
+
+class Border:
+    """Inputs of one call, and what the definitions give for them."""
+
+    def __init__(self, m, d, kind, post, pre, gate, sig, vectors, dtype, stream, seed=0, pitch=0, at=0, join=True, mean=0.0):
+        gen = torch.Generator().manual_seed(1000 * m + d + seed)
+        self.m, self.d, self.kind, self.post, self.pre, self.join = m, d, kind, post, pre, join
+        rnd = lambda *s: torch.randn(*s, generator=gen, dtype=torch.float64)  # noqa: E731
+        self.bufs = []
+
+        def rows(dt, x):
+            ld = pitch or d
+            buf = torch.full((m * ld + at + 16,), 5.0, dtype=DT[dt], device="cuda")
+            t = buf[at:at + m * ld].view(m, ld)[:, :d]
+            t.copy_(x)
+            return t
+
+        x = rnd(m, d) + mean
+        x[:, ::29] *= 12.0
+        self.R, self.dY, self.dN = rows(stream, x), rows(stream, rnd(m, d)), rows(dtype, rnd(m, d))
+        self.F = rows(dtype, rnd(m, d) + mean)
+        self.out = {k: rows(t, torch.zeros(m, d)) for k, t in (("Y", stream), ("N", dtype), ("R", stream), ("F", dtype))}
+        self.gate = None if gate is None else rnd(m).to(DT[dtype]).cuda() if gate == "row" else rows(dtype, rnd(m, d))
+        vec = lambda on, c: (c + 0.3 * rnd(d)).float().cuda() if on and vectors else None  # noqa: E731
+        self.vec = {"post_weight": vec(post, 1), "post_bias": vec(post, 0), "scale": vec(join, 0.5), "pre_weight": vec(pre, 1),
+                    "pre_bias": vec(pre, 0)}
+        self.alpha, self.sig = 0.75, sig
+        self.h = binding.BlockNorm(d, kind=kind, join=join, pre=pre, post=post, gate=gate, gate_act="sigmoid" if sig else None, eps=EPS,
+                                   dtype=dtype, stream_dtype=stream)
+        w = lambda t: None if t is None else t.double().cpu()  # noqa: E731
+        self.w = {k: w(t) for k, t in {**self.vec, "R": self.R, "F": self.F, "gate": self.gate, "dY": self.dY, "dN": self.dN}.items()}
+
+    def call(self):
+        kw = dict(self.vec, alpha=self.alpha)
+        if self.join:
+            kw.update(F=self.F, gate=self.gate)
+        return kw
+
+    def factor(self, v):
+        """alpha * scale * gate."""
+        f = torch.full((self.m, self.d), self.alpha, dtype=torch.float64)
+        if v["scale"] is not None:
+            f = f * v["scale"]
+        if v["gate"] is not None:
+            g = torch.sigmoid(v["gate"]) if self.sig else v["gate"]
+            f = f * (g[:, None] if g.dim() == 1 else g)
+        return f
+
+    def branch(self, v):
+        return norm(v["F"], self.kind, v["post_weight"], v["post_bias"]) if self.post else v["F"]
+
+    def check_forward(self, y, n):
+        w = self.w
+        if not self.join:
+            want, size = w["R"], torch.zeros_like(w["R"])
+        else:
+            want = w["R"] + self.factor(w) * self.branch(w)
+            v = norm_size(w["F"], self.kind, w["post_weight"], w["post_bias"]) if self.post else w["F"].abs()
+            size = w["R"].abs() + self.factor(w).abs() * v
+            near(y, want, size, "Y")
+        if self.pre:
+            # (Y's own error comes through the norm as a gradient does)
+            near(n, norm(want, self.kind, w["pre_weight"], w["pre_bias"]),
+                 norm_size(want, self.kind, w["pre_weight"], w["pre_bias"]) +
+                 through(want, self.kind, size) * (1 if w["pre_weight"] is None else w["pre_weight"].abs()), "N")
+
+    def check_backward(self, y, got, dy=True):
+        w = self.w
+        y = y.double().cpu()
+        leaf = lambda t: None if t is None else t.clone().requires_grad_(True)  # noqa: E731
+        T = w["dY"].clone() if dy else torch.zeros_like(y)
+        size = T.abs()
+        if self.pre:
+            yl, pw, pb = leaf(y), leaf(w["pre_weight"]), leaf(w["pre_bias"])
+            xs = [t for t in (yl, pw, pb) if t is not None]
+            gr = list(torch.autograd.grad(norm(yl, self.kind, pw, pb), xs, w["dN"]))
+            T = T + gr.pop(0)
+            h = w["dN"] if pw is None else w["dN"] * w["pre_weight"]
+            size = size + through(y, self.kind, h)
+            if pw is not None:
+                near(got["pre_weight"], gr.pop(0), (w["dN"].abs() * norm_size(y, self.kind)).sum(0), "pre_weight", 2 * U)
+            if pb is not None:
+                near(got["pre_bias"], gr.pop(0), w["dN"].abs().sum(0), "pre_bias", 2 * U)
+        near(got["R"], T, size, "dR")
+        if not self.join:
+            return
+        v = {k: leaf(t) for k, t in w.items()}
+        names = [k for k in ("F", "gate", "post_weight", "post_bias", "scale") if v[k] is not None]
+        gr = dict(zip(names, torch.autograd.grad(self.factor(v) * self.branch(v), [v[k] for k in names], T)))
+        vs = norm_size(w["F"], self.kind) if self.post else w["F"].abs()           # V
+        nb = norm_size(w["F"], self.kind, w["post_weight"], w["post_bias"]) if self.post else vs
+        fac = self.factor(w).abs()
+        bare = self.factor(dict(w, scale=None)).abs()
+        e = size * fac * (1 if w["post_weight"] is None else w["post_weight"].abs())
+        near(got["F"], gr["F"], through(w["F"], self.kind, e) if self.post else e, "dF")
+        if "gate" in gr:
+            one = dict(w, gate=None)
+            k = size * self.factor(one).abs() * nb      # (a sigmoid's slope is at most its gate)
+            k = k.sum(1) if w["gate"].dim() == 1 else k
+            near(got["gate"], gr["gate"], k, "dgate")
+        if "post_weight" in gr:
+            near(got["post_weight"], gr["post_weight"], (size * fac * vs).sum(0), "post_weight", 2 * U)
+            near(got["post_bias"], gr["post_bias"], (size * fac).sum(0), "post_bias", 2 * U)
+        if "scale" in gr:
+            near(got["scale"], gr["scale"], (size * bare * nb).sum(0), "scale", 2 * U)
+
+
+FORMS = [  # kind, post, pre, gate, sigmoid, vectors
+    ("rms", True, True, None, False, True), ("rms", True, True, "element", True, True), ("layer", True, True, "row", True, True),
+    ("layer", True, True, "element", False, True), ("rms", False, True, "row", False, True), ("layer", False, True, None, False, False),
+    ("rms", True, False, "element", False, True), ("layer", True, False, "row", False, False), ("rms", False, False, "element", True, True),
+    ("rms", False, False, None, False, False)]
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype,stream,m,d,pitch,at", [("bf16", "bf16", 1, 8, 0, 0), ("bf16", "f32", 37, 264, 272, 8), ("f32", "bf16", 5, 1000, 0, 0),
+                                                       ("bf16", "bf16", 9, 333, 335, 1), ("f32", "f32", 3, 1, 0, 0)])
+def test_border_and_its_gradients(form, dtype, stream, m, d, pitch, at):
+    kind, post, pre, gate, sig, vectors = form
+    b = Border(m, d, kind, post, pre, gate, sig, vectors, dtype, stream, pitch=pitch, at=at)
+    y, n = b.h.forward(b.R, **b.call(), out=b.out["Y"], normed=b.out["N"] if pre else None)
+    b.check_forward(y, n)
+    got = b.h.backward(y, dY=b.dY, dN=b.dN if pre else None, **b.call(), out={"R": b.out["R"], "F": b.out["F"]})
+    b.check_backward(y, got)
+    if pre:
+        b.check_backward(y, b.h.backward(y, dN=b.dN, **b.call()), dy=False)
+    again = b.h.backward(y, dY=b.dY, dN=b.dN if pre else None, **b.call())
+    for k in got:
+        assert torch.equal(got[k], again[k]), k                       # bitwise repeatable
+    for t in (b.R, b.F, b.out["Y"], b.out["R"]):                      # nothing between the rows was touched
+        base = t._base if t._base is not None else t
+        while base._base is not None:
+            base = base._base
+        edge = torch.ones_like(base, dtype=torch.bool)
+        edge[at:at + m * (pitch or d)].view(m, -1)[:, :d] = False
+        assert bool((base[edge] == 5.0).all())
+    assert b.h.last_status() == 0
+
+
+@pytest.mark.parametrize("kind,dtype,stream,m,d", [("rms", "bf16", "bf16", 1999, 768), ("layer", "bf16", "f32", 700, 2048), ("rms", "f32", "f32", 300, 4096),
+                                                   ("layer", "f32", "f32", 310, 8192), ("rms", "bf16", "bf16", 450, 7168), ("layer", "bf16", "bf16", 160, 4104),
+                                                   ("rms", "bf16", "f32", 155, 5003), ("layer", "bf16", "bf16", 2001, 96)])
+def test_many_rows(kind, dtype, stream, m, d):
+    """More rows than a grid takes at once, every width of a thread's share, stages that wrap."""
+    b = Border(m, d, kind, True, True, "element", True, True, dtype, stream)
+    y, n = b.h.forward(b.R, **b.call())
+    b.check_forward(y, n)
+    b.check_backward(y, b.h.backward(y, dY=b.dY, dN=b.dN, **b.call()))
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("m,d,mean", [(1, 2048, 0.0), (70, 640, 0.0), (33, 1001, 30.0)])
+def test_plain_norm_without_a_block(kind, m, d, mean):
+    """No F: Y is R.  A mean far from zero is taken off before the squares are added."""
+    b = Border(m, d, kind, False, True, None, False, True, "bf16", "f32", join=False, mean=mean)
+    kw = {k: b.vec[k] for k in ("pre_weight", "pre_bias")}
+    y, n = b.h.forward(b.R, **kw)
+    assert y is b.R
+    b.check_forward(y, n)
+    b.check_backward(y, b.h.backward(y, dY=b.dY, dN=b.dN, **kw))
+
+
+def test_gradients_against_differences():
+    """Central differences of the forward pass, in the direction of each operand."""
+    b = Border(6, 48, "layer", True, True, "row", True, True, "f32", "f32")
+    cy, cn = torch.randn(6, 48, device="cuda"), torch.randn(6, 48, device="cuda")
+
+    def value(**change):
+        kw = dict(b.call(), **{k: v for k, v in change.items() if k != "R"})
+        y, n = b.h.forward(change.get("R", b.R), **kw)
+        return float((y.double() * cy).sum() + (n.double() * cn).sum())
+
+    y, _ = b.h.forward(b.R, **b.call())
+    got = b.h.backward(y, dY=cy, dN=cn, **b.call())
+    h = 2.0 ** -7
+    for k in ("R", "F", "gate", "post_weight", "post_bias", "scale", "pre_weight", "pre_bias"):
+        x = b.R if k == "R" else b.call()[k]
+        step = torch.randn(x.shape, device="cuda")
+        slope = (value(**{k: x + h * step}) - value(**{k: x - h * step})) / (2 * h)
+        want = float((got[k].double() * step).sum())
+        # the sum of 576 products of fp32 results of size < 10 is off by < 576 * 10 * 2^-22 / h; third differences add h^2 times a few
+        # hundred times the slope's size at most
+        size = float((got[k].double().abs() * step.abs()).sum())
+        assert abs(slope - want) <= 576 * 10 * 2.0 ** -22 / h + 40 * h * h * size, k
+
+
+def test_rows_in_place():
+    b = Border(50, 512, "rms", True, True, "element", False, True, "bf16", "bf16")
+    y, n = b.h.forward(b.R, **b.call())
+    want = b.h.backward(y, dY=b.dY, dN=b.dN, **b.call())
+    r, f = b.R.clone(), b.F.clone()
+    y2, n2 = b.h.forward(r, **dict(b.call(), F=f), out=r, normed=f)
+    assert y2 is r and torch.equal(y2, y) and torch.equal(n2, n)
+    dy, dn, g = b.dY.clone(), b.dN.clone(), b.gate.clone()
+    got = b.h.backward(y, dY=dy, dN=dn, **dict(b.call(), gate=g), out={"R": dy, "F": dn, "gate": g})
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+
+
+def test_infinities_and_nans_stay_in_their_rows():
+    b = Border(20, 256, "layer", True, True, "row", False, True, "f32", "f32")
+    y0, n0 = b.h.forward(b.R, **b.call())
+    b.R[3, 7], b.F[11, 0], b.gate[17] = math.inf, math.nan, math.inf
+    y, n = b.h.forward(b.R, **b.call())
+    rest = [r for r in range(20) if r not in (3, 11, 17)]
+    assert torch.equal(y[rest], y0[rest]) and torch.equal(n[rest], n0[rest])
+    assert bool(n[3].isnan().any()) and bool(y[11].isnan().all()) and not bool(torch.isfinite(y[17]).any())
+
+
+def test_zero_rows_and_constant_rows():
+    b = Border(4, 64, "layer", True, True, None, False, False, "f32", "f32")
+    b.R.zero_()
+    b.F.fill_(3.0)
+    y, n = b.h.forward(b.R, **dict(b.call()))
+    assert bool((y == 0).all()) and bool((n == 0).all())
+    got = b.h.backward(y, dY=b.dY, dN=b.dN, **b.call())
+    assert all(bool(torch.isfinite(t).all()) for t in got.values())
+
+
+def test_empty_batch():
+    b = Border(1, 64, "rms", True, True, None, False, True, "bf16", "bf16")
+    e = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    before = binding.launch_count()
+    y, n = b.h.forward(e, **dict(b.call(), F=e))
+    assert y.shape == n.shape == (0, 64) and binding.launch_count() == before
+    got = b.h.backward(e, dY=e, dN=e, **dict(b.call(), F=e))
+    for k in ("post_weight", "scale", "pre_weight", "pre_bias"):
+        assert bool((got[k] == 0).all())
+
+
+def test_replayed_graph_and_another_stream():
+    b = Border(300, 768, "rms", True, True, "row", True, True, "bf16", "bf16")
+    y, n = b.h.forward(b.R, **b.call())
+    want = b.h.backward(y, dY=b.dY, dN=b.dN, **b.call())
+    ws = torch.empty(b.h.workspace_bytes(), dtype=torch.uint8, device="cuda")
+    out = {k: torch.zeros_like(v) for k, v in want.items()}
+    y2, n2 = torch.zeros_like(y), torch.zeros_like(n)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        b.h.forward(b.R, **b.call(), out=y2, normed=n2)
+        b.h.backward(y2, dY=b.dY, dN=b.dN, **b.call(), out=out, workspace=ws)
+    ws.fill_(255)
+    for _ in range(2):
+        for v in out.values():
+            v.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y2, y) and torch.equal(n2, n)
+        for k in want:
+            assert torch.equal(out[k], want[k]), k
+
+
+def test_refusals():
+    h = binding.BlockNorm(64, join=True, post=True, gate="element")
+    x = lambda: torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    w = torch.ones(64, device="cuda")
+    before = binding.launch_count()
+    for bad in (dict(F=x()), dict(gate=x()), dict(F=x(), gate=torch.zeros(4, device="cuda").bfloat16()), dict(F=x()[:, :63], gate=x()),
+                dict(F=x().float(), gate=x()), dict(F=x().cpu(), gate=x()), dict(F=x(), gate=x(), post_weight=w[:63]),
+                dict(F=x(), gate=x(), post_weight=w.bfloat16())):
+        with pytest.raises((ValueError, IndexError, binding.AlgError)):
+            h.forward(x(), **bad)
+    wide = torch.zeros(4, 96, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(binding.AlgError) as e:
+        h.forward(wide[:, :64], F=x(), gate=x(), out=wide[:, 32:])    # overlaps, but is not the same
+    assert e.value.code == 1
+    r = x()
+    with pytest.raises(binding.AlgError):
+        h.forward(r, F=x(), gate=x(), out=r, normed=r)                # two outputs in one place
+    with pytest.raises(binding.AlgError) as e:
+        h.backward(x(), dY=x(), dN=x(), F=x(), gate=x(), post_weight=w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == 3
+    with pytest.raises(binding.AlgError):
+        h.backward(x(), dY=x(), F=x(), gate=x())                      # a PRE handle needs dN
+    plain = binding.BlockNorm(64)
+    with pytest.raises(binding.AlgError):
+        plain.forward(x(), F=x())
+    with pytest.raises(ValueError):
+        plain.backward(x(), dN=x(), want=["nothing"])
+    assert binding.launch_count() == before
+    for kw in (dict(D=0), dict(D=64, pre=False), dict(D=64, post=True), dict(D=64, join=True, gate_act="sigmoid"), dict(D=64, eps=-1.0)):
+        with pytest.raises(binding.AlgError) as e:
+            binding.BlockNorm(**kw)
+        assert e.value.code == 1
+    with pytest.raises(binding.AlgError) as e:
+        binding.BlockNorm(8193)
+    assert e.value.code == 2
