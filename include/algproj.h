@@ -41,6 +41,7 @@ extern "C" {
 typedef struct alg_proj_s *alg_proj_t;
 typedef struct alg_ffn_s *alg_ffn_t;
 typedef struct alg_proj_grad_s *alg_proj_grad_t;
+typedef struct alg_moe_s *alg_moe_t;
 typedef struct alg_norm_s *alg_norm_t;
 typedef struct alg_ckpt_s *alg_ckpt_t;
 
@@ -363,6 +364,37 @@ alg_status_t alg_proj_grad_weight(alg_proj_grad_t h, const void *X, int64_t ldx,
                                   int64_t lddw, alg_dtype_t w_dtype, void *workspace,
                                   size_t workspace_bytes, void *stream);
 alg_status_t alg_proj_grad_last_status(alg_proj_grad_t h, void *stream, alg_status_t *status);
+
+/* ---- mixture of experts on a few tokens (serving) ------------------------------------------------------
+ * The gated FFN whose weights each row chooses itself: with logits L = X W_router (X: M x D bf16, W_router: D x E packed, of
+ * router_dtype) and scores P = softmax(L) over the E experts (SOFTMAX) or sigmoid(L) (SIGMOID), a row takes the top_k experts
+ * with the largest P + select_bias (E fp32 values or NULL; equal ones in ascending order of the expert), with weights P, divided by
+ * their sum if `renormalise` (a sum below 1e-20 counts as that), times route_scale:
+ *     Y = sum_j weight_j * (silu(X W_gate[e_j]) .* (X W_up[e_j])) W_down[e_j]
+ * W_gate_up: E banks [W_gate | W_up], each D x 2F packed; W_down: E banks F x D packed; all bf16.  Scores and sums are fp32; the
+ * weighted hidden rows are held as two bf16 terms (16 significant bits) for a bf16 Y, as three (24) for an fp32 Y.
+ * An expert whose select_bias is -infinity or NaN is never taken; a row that finds fewer than top_k experts has index -1 and weight 0
+ * in the places left, and Y = 0 where it finds none.  A row with a logit that is infinite or NaN takes no expert: index -1, weight NaN, Y NaN.
+ * `experts` (int32) and `weights` (fp32), both M x top_k packed, or NULL: the choice, best first.
+ * 1 <= M <= ALG_MOE_MAX_M; D and F multiples of 8; E <= ALG_MOE_MAX_EXPERTS, top_k <= ALG_MOE_MAX_TOP_K; X, Y and the weights on 16 bytes, ldx in
+ * multiples of 8, ldy of 16 bytes.  M = 0 is a successful no-op.  Only the experts that some row takes are read.  Two launches, no host
+ * synchronisation.  Calls on one handle must be ordered on the GPU (each launch's CTAs count in memory of the handle which of
+ * them is the last of a tile); calls of different handles may overlap.  No CTA waits for another cluster's.  Nothing is read ahead
+ * of the previous kernel's end.  Y may not overlap any operand.  Workspace: alg_moe_workspace_bytes(h, M), 256-byte aligned, no
+ * initialisation needed. */
+typedef enum { ALG_MOE_SOFTMAX = 0, ALG_MOE_SIGMOID = 1 } alg_moe_score_t;
+#define ALG_MOE_MAX_M 64
+#define ALG_MOE_MAX_EXPERTS 512
+#define ALG_MOE_MAX_TOP_K 32
+alg_status_t alg_moe_create(alg_moe_t *out, int D, int F, int E, int top_k, alg_moe_score_t score, int renormalise, float route_scale,
+                            alg_dtype_t router_dtype);
+alg_status_t alg_moe_destroy(alg_moe_t h);
+alg_status_t alg_moe_workspace_bytes(alg_moe_t h, int64_t max_M, size_t *bytes);
+alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M, const void *W_router, const float *select_bias,
+                             const void *W_gate_up, const void *W_down, void *Y, int64_t ldy, alg_dtype_t y_dtype, int32_t *experts,
+                             float *weights, void *workspace, size_t workspace_bytes, void *stream);
+/* Reads and clears the handle's device status word, as alg_proj_last_status. */
+alg_status_t alg_moe_last_status(alg_moe_t h, void *stream, alg_status_t *status);
 
 /* ---- a block's border: norms before and after a block, with its gate and residual scale ----------------
  * With the block's output F and the residual stream R (both M x D), in one pass:

@@ -24,6 +24,7 @@ ALG_SCHED_EXPLICIT, ALG_SCHED_CYCLIC, ALG_SCHED_INTERVAL = 0, 1, 2
 ALG_Q8_E4M3, ALG_Q8_INT8 = 0, 1
 ALG_NORM_RMS, ALG_NORM_LAYER = 0, 1
 ALG_NORM_JOIN, ALG_NORM_PRE, ALG_NORM_POST, ALG_NORM_GATE_ROW, ALG_NORM_GATE_ELEMENT, ALG_NORM_GATE_SIGMOID = 1, 2, 4, 8, 16, 32
+ALG_MOE_SOFTMAX, ALG_MOE_SIGMOID = 0, 1
 ALG_PATH_SIMT, ALG_PATH_TCGEN05, ALG_PATH_DECODE = 0, 1, 2
 OPTIONS = {"gemm_kernel": 1, "tile_n": 2, "small_m_kernel": 3, "host_plan": 4, "wait_limit_cycles": 5,
            "test_stall_bytes": 6, "stage_k": 7, "interval_period": 8, "row_gather": 9, "weight_packed": 10}
@@ -42,6 +43,7 @@ EXPORTS = [
     "alg_ffn_workspace_bytes", "alg_ffn_forward", "alg_ffn_host_workspace_bytes", "alg_ffn_forward_host",
     "alg_ffn_gated_create", "alg_ffn_gated_forward", "alg_proj_grad_create", "alg_proj_grad_destroy",
     "alg_proj_grad_workspace_bytes", "alg_proj_grad_input", "alg_proj_grad_weight", "alg_proj_grad_last_status", "alg_ffn_macs", "alg_ffn_last_status", "alg_ffn_set_timing", "alg_ffn_get_timing", "alg_status_string", "alg_launch_count",
+    "alg_moe_create", "alg_moe_destroy", "alg_moe_workspace_bytes", "alg_moe_forward", "alg_moe_last_status",
     "alg_norm_create", "alg_norm_destroy", "alg_norm_workspace_bytes", "alg_norm_forward", "alg_norm_backward", "alg_norm_last_status",
     "alg_ckpt_create", "alg_ckpt_destroy", "alg_ckpt_row_bytes", "alg_ckpt_store", "alg_ckpt_load", "alg_ckpt_act_forward",
     "alg_ckpt_act_backward",
@@ -99,6 +101,11 @@ def lib() -> ctypes.CDLL:
         L.alg_ffn_last_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         L.alg_ffn_set_timing.argtypes = [vp, i32]
         L.alg_ffn_get_timing.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
+        L.alg_moe_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, i32, i32, i32, ctypes.c_float, i32]
+        L.alg_moe_destroy.argtypes = [vp]
+        L.alg_moe_workspace_bytes.argtypes = [vp, i64, ctypes.POINTER(ctypes.c_size_t)]
+        L.alg_moe_forward.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, vp, i64, i32, vp, vp, vp, ctypes.c_size_t, vp]
+        L.alg_moe_last_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         L.alg_norm_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, ctypes.c_float, i32, i32]
         L.alg_norm_destroy.argtypes = [vp]
         L.alg_norm_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
@@ -443,6 +450,65 @@ class ProjGrad(_Handle):
     def last_status(self, stream=None) -> int:
         s = ctypes.c_int()
         _check(lib().alg_proj_grad_last_status(self._h, _stream(stream), ctypes.byref(s)), "alg_proj_grad_last_status")
+        return s.value
+
+
+class MoE(_Handle):
+    """alg_moe_* : Y = sum_j weight_j * (silu(X W_gate[e_j]) .* (X W_up[e_j])) W_down[e_j], the experts e_j of a row chosen by
+    its router scores.  W_router: D x E (``router_dtype``); W_gate_up: E x D x 2F, [W_gate | W_up]; W_down: E x F x D."""
+    _destroy = "alg_moe_destroy"
+
+    def __init__(self, D, F, experts, top_k, score="softmax", renormalise=True, route_scale=1.0, router_dtype="bf16"):
+        super().__init__()
+        self.D, self.F, self.E, self.top_k = int(D), int(F), int(experts), int(top_k)
+        self.router_type = torch.float32 if _DTYPES[router_dtype] == ALG_F32 else torch.bfloat16
+        _check(lib().alg_moe_create(ctypes.byref(self._h), self.D, self.F, self.E, self.top_k,
+                                    {"softmax": ALG_MOE_SOFTMAX, "sigmoid": ALG_MOE_SIGMOID}[score], int(bool(renormalise)), float(route_scale),
+                                    _DTYPES[router_dtype]), "alg_moe_create")
+        self._device = torch.cuda.current_device()
+
+    def set_option(self, name, value):
+        raise NotImplementedError("mixture-of-experts handles have no options")
+
+    def workspace_bytes(self, max_M: int) -> int:
+        out = ctypes.c_size_t()
+        _check(lib().alg_moe_workspace_bytes(self._h, max_M, ctypes.byref(out)), "alg_moe_workspace_bytes")
+        return out.value
+
+    def _packed(self, t, what, shape, dtype):
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._device or not t.is_contiguous():
+            raise ValueError(f"{what} must be a packed {shape} {dtype} tensor on the handle's device")
+        return t.data_ptr()
+
+    def forward(self, X, W_router, W_gate_up, W_down, select_bias=None, out=None, out_dtype=None, routing=False, experts=None, weights=None,
+                workspace=None, stream=None):
+        """Y, or (Y, experts, weights) with ``routing``: the rows' experts (int32) and their weights (fp32), M x top_k."""
+        M = X.shape[0]
+        ldx = _rows(X, "X", M, self.D, torch.bfloat16, self._device)
+        if M > 64:
+            raise AlgError(2, "alg_moe_forward")
+        if out is None:
+            out = torch.empty((M, self.D), dtype=out_dtype or X.dtype, device=X.device)
+            ldo = self.D
+        else:
+            ldo = _rows(out, "out", M, self.D, out.dtype, self._device)
+        if routing:
+            experts = torch.empty((M, self.top_k), dtype=torch.int32, device=X.device) if experts is None else experts
+            weights = torch.empty((M, self.top_k), dtype=torch.float32, device=X.device) if weights is None else weights
+        pairs = (M, self.top_k)
+        ws = workspace if workspace is not None else self._own_workspace(M, X.device)
+        _check(lib().alg_moe_forward(self._h, X.data_ptr(), ldx, M, self._packed(W_router, "W_router", (self.D, self.E), self.router_type),
+                                     None if select_bias is None else self._packed(select_bias, "select_bias", (self.E,), torch.float32),
+                                     self._packed(W_gate_up, "W_gate_up", (self.E, self.D, 2 * self.F), torch.bfloat16),
+                                     self._packed(W_down, "W_down", (self.E, self.F, self.D), torch.bfloat16), out.data_ptr(), ldo,
+                                     _DTYPES[out.dtype], None if experts is None else self._packed(experts, "experts", pairs, torch.int32),
+                                     None if weights is None else self._packed(weights, "weights", pairs, torch.float32), _ptr(ws), ws.numel(),
+                                     _stream(stream)), "alg_moe_forward")
+        return (out, experts, weights) if routing else out
+
+    def last_status(self, stream=None) -> int:
+        s = ctypes.c_int()
+        _check(lib().alg_moe_last_status(self._h, _stream(stream), ctypes.byref(s)), "alg_moe_last_status")
         return s.value
 
 

@@ -42,3 +42,19 @@ def test_norm_handles_refuse_bad_arguments_first():
                                None, None, None, None, None, 0, None) == 1
     s = ctypes.c_int()
     assert L.alg_norm_last_status(None, None, ctypes.byref(s)) == 1
+
+
+def test_expert_handles_refuse_bad_arguments_first():
+    L, h = _lib(), ctypes.c_void_p()
+    ref = ctypes.byref(h)
+    assert L.alg_moe_create(None, 64, 64, 8, 2, 0, 1, 1.0, 1) == 1
+    for code, args in ((1, (0, 64, 8, 2, 0, 1, 1.0, 1)), (1, (64, 0, 8, 2, 0, 1, 1.0, 1)), (1, (64, 64, 0, 1, 0, 1, 1.0, 1)), (1, (64, 64, 8, 9, 0, 1, 1.0, 1)),
+                       (1, (64, 64, 8, 0, 0, 1, 1.0, 1)), (1, (64, 64, 8, 2, 2, 1, 1.0, 1)), (1, (64, 64, 8, 2, 0, 1, float("nan"), 1)),
+                       (1, (64, 64, 8, 2, 0, 1, 1.0, 2)), (2, (60, 64, 8, 2, 0, 1, 1.0, 1)), (2, (64, 4, 8, 2, 0, 1, 1.0, 1)),
+                       (2, (64, 64, 513, 2, 0, 1, 1.0, 1)), (2, (64, 64, 64, 33, 0, 1, 1.0, 1))):
+        assert L.alg_moe_create(ref, *args) == code, args
+        assert not h.value
+    n, s = ctypes.c_size_t(), ctypes.c_int()
+    assert L.alg_moe_workspace_bytes(None, 1, ctypes.byref(n)) == 1 and L.alg_moe_destroy(None) == 1
+    assert L.alg_moe_forward(None, None, 0, 1, None, None, None, None, None, 0, 1, None, None, None, 0, None) == 1
+    assert L.alg_moe_last_status(None, None, ctypes.byref(s)) == 1
