@@ -3,20 +3,22 @@
 // First launch: router, choice of the experts, gate and up products, silu(gate) * up * weight.  Second: down products and the
 // sum over a row's experts.  Bound by HBM: every weight of a chosen expert is read once and used for all its rows.
 //
-// Router.  The CTAs of a thread-block cluster share the logits: each takes E / cluster experts and hands them to its peers through
-// distributed shared memory.  Every cluster does that for itself (the router is read from L2), so no CTA waits for
-// another cluster, and every CTA knows the choice without a launch of its own for it.
+// Router.  The CTAs of a thread-block cluster share the logits: each reduces over an eighth of D (a quarter, for half of more than 256
+// experts), adds up its peers' parts of every eighth row through distributed shared memory, chooses that row's experts and
+// tells its peers.  Every cluster does that for itself (the router is read from L2), so no CTA waits for another cluster, and every CTA
+// knows the choice without a launch of its own for it.  An fp32 router is taken as three bf16 terms, which hold all its bits.
 //
-// Products.  A unit is 128 columns of one expert's bank (64 gate and the matching 64 up ones) or, for the down product, 128
-// columns of Y over all chosen experts; its reduction is cut into chunks of 64 weight rows.  The chunks of all units in a row are
-// dealt to the CTAs in equal consecutive shares, whatever the number of experts and rows.  A unit that lies in one CTA is finished there.
-// The others leave their partial sums in the workspace, and whichever CTA counts itself the last of a unit adds them in CTA order (so the
-// sums are the same every time) and finishes it: nobody waits.
+// Products.  A unit is 128 gate and the matching 128 up columns of one expert's bank or, for the down product, 256
+// columns of Y over all chosen experts; its reduction is cut into chunks of 64 weight rows (32 KB).  The chunks of all units in a row
+// are dealt to the CTAs in equal consecutive shares, whatever the number of experts and rows.  A unit that lies in one CTA is finished
+// there.  The others leave their partial sums in the workspace, and whichever CTA counts itself the last of a unit adds them in CTA
+// order (so the sums are the same every time) and finishes it: nobody waits.
 //
-// Weights come by tiled copies (64 x 64 boxes, 128-byte swizzle) through a ring of stages that one thread keeps full; eight warps
-// multiply with mma.sync, weights as the 16-row operand, eight rows of X a step.  The tensor pipe has slack: at 16 KB in
-// about 700 cycles a chunk needs 32 of its products per 8 rows.  A chunk's sums start at zero and are added to the unit's in
-// fp32, so the length of the chains inside the tensor core does not grow with D.
+// Weights come by tiled copies (boxes of 64 columns, 128-byte swizzle) through a ring of stages.  What limits such a stream is the
+// thread that asks for it, about 150 cycles a copy: with 16 KB in two copies 5.5 TB/s, 32 KB in one copy 6.6 to 7.1 (gate and up
+// boxes of two column blocks are one 5-D box), 8 KB rows 3.5.  So one warp asks for weights, another for the rows they
+// multiply.  Eight warps multiply with mma.sync, weights as the 16-row operand, eight rows a step; a chunk's sums start at zero and are
+// added to the unit's in fp32, so the length of the chains inside the tensor core does not grow with D.
 #include <cfloat>
 #include <cmath>
 #include <new>
@@ -44,13 +46,15 @@ namespace {
 
 using namespace tc;
 
-constexpr int kWarps = 8, kConsumers = kWarps * 32, kThreads = kConsumers + 32;
-constexpr int kCluster = 4;
-constexpr int kStages = 12;                 // at most
-constexpr int kBox = 64 * 64 * 2;           // one box of weights
+constexpr int kWarps = 8, kConsumers = kWarps * 32, kThreads = kConsumers + 64;   // two warps fetch
+constexpr int kCluster = 8;
+constexpr int kStages = 6;                  // at most
+constexpr int kBox = 64 * 64 * 2;           // 64 columns of 64 rows of weights
+constexpr int kChunk = 4 * kBox;            // up: [column block][gate, up]; down: [column block]
+constexpr int kUpCols = 128, kDownCols = 256;
 constexpr int kSmemLimit = 225 * 1024;
 constexpr int kMaxM = ALG_MOE_MAX_M;
-constexpr int kRouterRows = 4;              // rows of X at a time in the router's product
+constexpr int kLogitCols = 256;             // experts a CTA has logits of
 
 struct MoeArgs {
   int M, D, F, E, k, sigmoid, renormalise, y_f32, planes;
@@ -58,16 +62,17 @@ struct MoeArgs {
   const __nv_bfloat16 *X;
   int64_t ldx;
   const void *W_router;
-  int router_f32, router_vec;
+  int router_f32, router_copies;   // copies: the router's rows lie on 16 bytes and are bf16
   const float *bias;
   int32_t *experts;
   float *weights;
   void *Y;
   int64_t ldy;
-  int *route_idx;             // workspace: the choice, [M][k]
-  float *route_w;
-  __nv_bfloat16 *H;           // workspace: weighted hidden rows, [planes][M * k][F]
-  float4 *part;               // workspace: partial sums, [CTA][2][8 warps][row tiles][32 lanes]
+  int *table;                 // workspace: the chosen experts, as `Chosen` lies in shared memory
+  __nv_bfloat16 *H;           // workspace: weighted hidden rows, [planes][M * k][ldh]
+  int ldh;                    // F to the next multiple of 64
+  float4 *part;               // workspace: partial sums, [CTA][2][8 warps][2][row tiles][32 lanes]
+  int blocks;                 // tensor maps of whole column blocks (one copy a chunk)
   int *count;                 // [CTA]: arrivals at the unit whose first contributor it is
   int *status;
   long long wait_limit;
@@ -75,24 +80,39 @@ struct MoeArgs {
   int off_ring;               // the ring; in front of it what `Routes` points to
 };
 
-// The rows' choice, turned round: who takes an expert.
+// The chosen experts in ascending order: what both launches go by.
+struct Chosen {
+  int *n;          // how many
+  uint2 *mask;     // the rows that take them
+  int *expert;
+  int *first;      // [n + 1] their first pair
+  float *rest;     // [M] what the places without an expert add to a row: 0, or NaN
+  __device__ __forceinline__ Chosen(uint8_t *p, int most, int M) {
+    n = (int *)p, p += 8;
+    mask = (uint2 *)p, p += (size_t)most * 8;
+    expert = (int *)p, p += (size_t)most * 4;
+    first = (int *)p, p += (size_t)(most + 1) * 4;
+    rest = (float *)p;
+  }
+  __host__ __device__ static int words(int most, int M) { return 2 + 4 * most + 1 + M; }
+};
+// The rows' own choice; the first launch's.
 struct Routes {
-  int *idx;        // [M * k] experts of a row, -1 for none
-  float *w;        // [M * k]
   uint2 *mask;     // [E] the rows that take an expert
-  int *act;        // chosen experts in ascending order
-  int *first;      // [chosen + 1] their first pair
-  int *n_act;
+  int *idx;        // [M * k] experts of a row, -1 for none
+  float *w;        // [M * k] their weights
+  int *place;      // [E] among the chosen
+  float *pair_w;   // [M * k] weights in the order of the pairs
   __device__ __forceinline__ Routes(uint8_t *p, int P, int E) {
     mask = (uint2 *)p, p += (size_t)E * 8;
     idx = (int *)p, p += (size_t)P * 4;
     w = (float *)p, p += (size_t)P * 4;
-    act = (int *)p, p += (size_t)E * 4;
-    first = (int *)p, p += (size_t)(E + 1) * 4;
-    n_act = (int *)p;
+    place = (int *)p, p += (size_t)E * 4;
+    pair_w = (float *)p;
   }
-  static size_t bytes(int P, int E) { return (size_t)E * 16 + (size_t)P * 8 + 8; }
+  static size_t bytes(int P, int E) { return (size_t)E * 12 + (size_t)P * 12; }
 };
+__host__ __device__ __forceinline__ int most_chosen(int P, int E) { return P < E ? P : E; }
 __device__ __forceinline__ int rows_of(uint2 m) { return __popc(m.x) + __popc(m.y); }
 // Rows below `row` that take the expert.
 __device__ __forceinline__ int rows_below(uint2 m, int row) {
@@ -106,20 +126,26 @@ __device__ __forceinline__ int nth_row(uint2 m, int n) {   // n < rows_of(m)
   return __ffs(w) - 1 + (n < lo ? 0 : 32);
 }
 
-// From r.idx; all threads of the CTA.
-__device__ void turn_round(const Routes &r, int P, int E, int k) {
-  const int tid = threadIdx.x;
-  for (int e = tid; e < E; e += kThreads) r.mask[e] = make_uint2(0u, 0u);
-  __syncthreads();
+// From r.idx and r.w, with r.mask zero; all threads of the CTA.
+__device__ void turn_round(const Routes &r, const Chosen &ch, int M, int E, int k) {
+  const int tid = threadIdx.x, P = M * k;
   for (int p = tid; p < P; p += kThreads) {
     const int e = r.idx[p], m = p / k;
     if (e >= 0) atomicOr(m < 32 ? &r.mask[e].x : &r.mask[e].y, 1u << (m & 31));
+  }
+  for (int m = tid; m < M; m += kThreads) {
+    float s = 0.f;
+    for (int j = 0; j < k; ++j)
+      if (r.idx[m * k + j] < 0) s += r.w[m * k + j];
+    ch.rest[m] = s;
   }
   __syncthreads();
   if (tid < 32) {
     int n = 0, pairs = 0;
     for (int e0 = 0; e0 < E; e0 += 32) {
-      const int e = e0 + tid, c = e < E ? rows_of(r.mask[e]) : 0;
+      const int e = e0 + tid;
+      const uint2 mask = e < E ? r.mask[e] : make_uint2(0u, 0u);
+      const int c = rows_of(mask);
       const uint32_t used = __ballot_sync(~0u, c > 0);
       int sum = c;
 #pragma unroll
@@ -128,11 +154,16 @@ __device__ void turn_round(const Routes &r, int P, int E, int k) {
         if (tid >= o) sum += v;
       }
       const int at = n + __popc(used & ((1u << tid) - 1u));
-      if (c > 0) r.act[at] = e, r.first[at] = pairs + sum - c;
+      if (c > 0) ch.expert[at] = e, ch.mask[at] = mask, ch.first[at] = pairs + sum - c, r.place[e] = at;
       n += __popc(used);
       pairs += __shfl_sync(~0u, sum, 31);
     }
-    if (tid == 0) r.first[n] = pairs, *r.n_act = n;
+    if (tid == 0) ch.first[n] = pairs, *ch.n = n;
+  }
+  __syncthreads();
+  for (int p = tid; p < P; p += kThreads) {
+    const int e = r.idx[p], m = p / k;
+    if (e >= 0) r.pair_w[ch.first[r.place[e]] + rows_below(r.mask[e], m)] = r.w[p];
   }
   __syncthreads();
 }
@@ -148,100 +179,43 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Eight columns of the router, zero past the end.
-__device__ __forceinline__ void router8(const MoeArgs &a, int k, int e, int end, float (&w)[8]) {
-  if (a.router_vec) {
-    if (a.router_f32) {
-      Raw8<float> r;
-      r.load((const float *)a.W_router + (size_t)k * a.E + e);
-      r.get(w);
-    } else {
-      Raw8<__nv_bfloat16> r;
-      r.load((const __nv_bfloat16 *)a.W_router + (size_t)k * a.E + e);
-      r.get(w);
-    }
-    return;
+// Which part of the logits a CTA has: experts [e0, e0 + 256) over chunks [begin, end) of D.
+struct LogitShare {
+  int slices, e0, begin, end;
+  __device__ __forceinline__ LogitShare(const MoeArgs &a) {
+    const int rank = (int)cluster_rank(), chunks = (a.D + 63) / 64;
+    slices = a.E > kLogitCols ? kCluster / 2 : kCluster;
+    e0 = rank / slices * kLogitCols;
+    const int s = rank % slices;
+    begin = chunks * s / slices, end = chunks * (s + 1) / slices;
   }
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    w[c] = 0.f;
-    if (e + c < end)
-      w[c] = a.router_f32 ? ((const float *)a.W_router)[(size_t)k * a.E + e + c]
-                          : __bfloat162float(((const __nv_bfloat16 *)a.W_router)[(size_t)k * a.E + e + c]);
-  }
-}
-
-// Logits of all rows, [M][E], in every CTA of the cluster.  Eight columns a lane, eight rows of the router a step; the lanes of
-// a column group and the warps split D.
-__device__ void router_logits(const MoeArgs &a, float *logits, float *red) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int per = ((a.E + kCluster - 1) / kCluster + 7) / 8 * 8;
-  const int e0 = (int)cluster_rank() * per, en = max(0, min(per, a.E - e0));
-  int groups = 1;
-  while (groups * 8 < en) groups *= 2;
-  const int slots = 32 / groups, cg = lane & (groups - 1), slot = lane / groups;
-  const bool on = cg * 8 < en;
-  if (warp < kWarps && en > 0) {
-    for (int m0 = 0; m0 < a.M; m0 += kRouterRows) {
-      float acc[kRouterRows][8];
-#pragma unroll
-      for (int m = 0; m < kRouterRows; ++m)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) acc[m][c] = 0.f;
-      if (on)
-        for (int k0 = (warp * slots + slot) * 8; k0 < a.D; k0 += kWarps * slots * 8) {
-          float x[kRouterRows][8];
-#pragma unroll
-          for (int m = 0; m < kRouterRows; ++m) {
-            Raw8<__nv_bfloat16> r;
-            if (m0 + m < a.M) r.load(a.X + (int64_t)(m0 + m) * a.ldx + k0);
-            else r.zero();
-            r.get(x[m]);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float w[8];
-            router8(a, k0 + i, e0 + cg * 8, e0 + en, w);
-#pragma unroll
-            for (int m = 0; m < kRouterRows; ++m)
-#pragma unroll
-              for (int c = 0; c < 8; ++c) acc[m][c] = fmaf(x[m][i], w[c], acc[m][c]);
-          }
+};
+// A chunk of a router that tiled copies cannot fetch, as they would have left it; term p of an fp32 one.  All consumers.
+__device__ void fill_router(const MoeArgs &a, uint8_t *stage, int e0, int k0, int p) {
+  for (int i = threadIdx.x; i < 64 * kLogitCols; i += kConsumers) {
+    const int e = i & (kLogitCols - 1), k = i / kLogitCols;
+    __nv_bfloat16 v = __float2bfloat16_rn(0.f);
+    if (e0 + e < a.E && k0 + k < a.D) {
+      const size_t at = (size_t)(k0 + k) * a.E + e0 + e;
+      if (a.router_f32) {
+        float rest = ((const float *)a.W_router)[at];
+        v = __float2bfloat16_rn(rest);
+        for (int t = 0; t < p; ++t) {
+          const float back = __bfloat162float(v);
+          rest = isfinite(back) ? rest - back : 0.f;
+          v = __float2bfloat16_rn(rest);
         }
-      for (int o = groups; o < 32; o <<= 1)
-#pragma unroll
-        for (int m = 0; m < kRouterRows; ++m)
-#pragma unroll
-          for (int c = 0; c < 8; ++c) acc[m][c] += __shfl_xor_sync(~0u, acc[m][c], o);
-      if (slot == 0 && on)
-#pragma unroll
-        for (int m = 0; m < kRouterRows; ++m)
-#pragma unroll
-          for (int c = 0; c < 8; ++c) red[(warp * kRouterRows + m) * per + cg * 8 + c] = acc[m][c];
-      consumer_barrier();
-      for (int i = tid; i < kRouterRows * en; i += kConsumers) {
-        const int m = i / en, c = i - m * en;
-        if (m0 + m < a.M) {
-          float s = 0.f;
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) s += red[(w * kRouterRows + m) * per + c];
-          const uint32_t dst = smem_u32(logits + (size_t)(m0 + m) * a.E + e0 + c);
-#pragma unroll
-          for (uint32_t p = 0; p < kCluster; ++p) {
-            uint32_t there;
-            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(dst), "r"(p));
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(s) : "memory");
-          }
-        }
+      } else {
+        v = ((const __nv_bfloat16 *)a.W_router)[at];
       }
-      consumer_barrier();
     }
+    *(__nv_bfloat16 *)(stage + (e >> 6) * kBox + k * 128 + (((e & 63) * 2) ^ ((k & 7) << 4))) = v;
   }
 }
 
-// A warp chooses the experts of row m.  Without a bias the order is that of the logits, which a score that underflows or saturates
-// cannot spoil.
-__device__ void choose(const MoeArgs &a, const float *logits, const Routes &r, int m) {
+// A warp adds up the logits of row m and chooses its experts, for all CTAs of the cluster.  Without a bias the order is that of the
+// logits, which a score that underflows or saturates cannot spoil.
+__device__ void choose(const MoeArgs &a, const float *logits, int slices, const Routes &r, int m) {
   constexpr int kMost = ALG_MOE_MAX_EXPERTS / 32;
   const int lane = threadIdx.x & 31;
   float l[kMost], key[kMost];
@@ -249,16 +223,31 @@ __device__ void choose(const MoeArgs &a, const float *logits, const Routes &r, i
   float top = -FLT_MAX;
 #pragma unroll
   for (int i = 0; i < kMost; ++i) {
-    const int e = lane + 32 * i;
-    l[i] = e < a.E ? logits[(size_t)m * a.E + e] : 0.f;
+    l[i] = 0.f;
+    key[i] = -INFINITY;
+    if (32 * i >= a.E) continue;
+    const int e = min(lane + 32 * i, a.E - 1), first = e / kLogitCols * slices;
+    const uint32_t at = smem_u32(logits + m * kLogitCols + (e & (kLogitCols - 1)));
+    float part[kCluster];
+#pragma unroll
+    for (int p = 0; p < kCluster; ++p) {
+      uint32_t there;
+      part[p] = 0.f;
+      if (p < slices) {
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(first + p));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[p]) : "r"(there) : "memory");
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < kCluster; ++p) l[i] += part[p];
     bad = bad || !isfinite(l[i]);
-    if (e < a.E) top = fmaxf(top, l[i]);
+    top = fmaxf(top, l[i]);
   }
   bad = __any_sync(~0u, bad);
 #pragma unroll
   for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
   float sum = 1.f;
-  if (!a.sigmoid) {
+  if (!a.sigmoid && (a.bias || !a.renormalise)) {   // (else the sum cancels)
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kMost; ++i)
@@ -270,20 +259,19 @@ __device__ void choose(const MoeArgs &a, const float *logits, const Routes &r, i
 #pragma unroll
   for (int i = 0; i < kMost; ++i) {
     const int e = lane + 32 * i;
-    key[i] = -INFINITY;
     if (e < a.E) {
       key[i] = a.bias ? score(l[i]) + a.bias[e] : l[i];
       key[i] = key[i] == key[i] ? key[i] + 0.f : -INFINITY;   // (-0 is 0)
     }
   }
   int mine = -1;      // lane j keeps the j-th choice
-  float w = 0.f;
+  float w = 0.f, mine_l = 0.f;
   for (int j = 0; j < a.k && !bad; ++j) {
     float best = -INFINITY, at = 0.f;
     int e = 0x7FFFFFFF;
 #pragma unroll
     for (int i = 0; i < kMost; ++i)
-      if (key[i] > best) best = key[i], e = lane + 32 * i, at = l[i];
+      if (32 * i < a.E && key[i] > best) best = key[i], e = lane + 32 * i, at = l[i];
     const uint32_t bits = __float_as_uint(best), order = bits >> 31 ? ~bits : bits | 0x80000000u;
     const uint32_t most = __reduce_max_sync(~0u, order);
     const int win = (int)__reduce_min_sync(~0u, order == most ? (uint32_t)e : 0x7FFFFFFFu);
@@ -292,8 +280,9 @@ __device__ void choose(const MoeArgs &a, const float *logits, const Routes &r, i
 #pragma unroll
     for (int i = 0; i < kMost; ++i)
       if (lane + 32 * i == win) key[i] = -INFINITY;
-    if (lane == j) mine = win, w = score(at);
+    if (lane == j) mine = win, mine_l = at;
   }
+  if (mine >= 0) w = score(mine_l);
   if (a.renormalise) {
     float s = w;
 #pragma unroll
@@ -302,8 +291,15 @@ __device__ void choose(const MoeArgs &a, const float *logits, const Routes &r, i
   }
   w = bad ? __uint_as_float(0x7FC00000u) : w * a.route_scale;
   if (lane < a.k) {
-    r.idx[m * a.k + lane] = mine;
-    r.w[m * a.k + lane] = w;
+    const uint32_t idx_at = smem_u32(r.idx + m * a.k + lane), w_at = smem_u32(r.w + m * a.k + lane);
+#pragma unroll
+    for (uint32_t p = 0; p < kCluster; ++p) {
+      uint32_t there;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(idx_at), "r"(p));
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(mine) : "memory");
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(w_at), "r"(p));
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(w) : "memory");
+    }
   }
 }
 
@@ -345,7 +341,7 @@ __device__ __forceinline__ Ring make_ring(const MoeArgs &a, uint8_t *smem, uint6
 }
 __device__ __forceinline__ void init_ring(uint64_t *bars, int stages) {   // one thread
   const uint32_t full = smem_u32(bars), empty = full + 8 * kStages;
-  for (int s = 0; s < stages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, kWarps);
+  for (int s = 0; s < stages; ++s) mbar_init(full + 8 * s, 2), mbar_init(empty + 8 * s, kWarps);   // two warps fetch, eight use
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
 
@@ -364,12 +360,34 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&w)[4], uint3
                : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(b0), "r"(b1));
 }
 // Weights of a chunk, 16 columns of the warp by 64 rows: lanes 0-15 address rows 0-7 of the first and of the second eight
-// columns, lanes 16-31 rows 8-15; `lo` and `hi`: boxes and byte columns of the two eights.
+// columns, lanes 16-31 rows 8-15; `box` and `byte_col` are those of the lane's eight.
 __device__ __forceinline__ void load_weights(uint32_t box, int byte_col, uint32_t (&w)[4][4]) {
   const int lane = threadIdx.x & 31, row = (lane & 7) + (lane >> 4 << 3);
   const uint32_t at = box + row * 128 + (byte_col ^ ((row & 7) << 4));
 #pragma unroll
   for (int k = 0; k < 4; ++k) ldmatrix4_trans(at + k * 16 * 128, w[k]);
+}
+
+// Two tiles of sixteen columns by the eight rows a lane addresses its part of, added to acc[.][t].
+template <int NT>
+__device__ __forceinline__ void product(const uint32_t (&w)[2][4][4], uint32_t at, int sw, float (&acc)[2][NT][4], int t) {
+  const int lane = threadIdx.x & 31;
+  uint32_t b[4], c[4];
+  ldmatrix4(at + (((lane >> 3) * 16) ^ sw), b);
+  ldmatrix4(at + ((64 + (lane >> 3) * 16) ^ sw), c);
+  float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int j = 0; j < 2; ++j) mma(d[j], w[j][0], b[0], b[1]);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) mma(d[j], w[j][1], b[2], b[3]);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) mma(d[j], w[j][2], c[0], c[1]);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) mma(d[j], w[j][3], c[2], c[3]);
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[j][t][e] += d[j][e];
 }
 
 // The share of CTA c of n among `total` chunks, and whose share a chunk is in; n <= total, so that nobody's is empty (CTAs past n have none).
@@ -379,19 +397,21 @@ __device__ __forceinline__ int owner(int64_t total, int64_t chunk, int n) { retu
 // The sums of a unit that several CTAs have parts of: leaves this CTA's and, in the last to come, adds all of them in CTA order.
 // True in that CTA.  All consumers.
 template <int NT>
-__device__ bool meet_parts(const MoeArgs &a, float (&acc)[NT][4], int nt, int64_t total, int n, int per_unit, int64_t unit, int *flag) {
+__device__ bool meet_parts(const MoeArgs &a, float (&acc)[2][NT][4], int nt, int64_t total, int n, int per_unit, int64_t unit, int *flag) {
   const int me = blockIdx.x, tiles = (a.M + 7) / 8;
   const int c0 = owner(total, unit * per_unit, n), c1 = owner(total, (unit + 1) * per_unit - 1, n);
   if (c0 == c1) return true;
-  const size_t warp_at = (size_t)(threadIdx.x >> 5) * tiles * 32 + (threadIdx.x & 31), slot = (size_t)kWarps * tiles * 32;
-  auto part_of = [&](int c) {   // a CTA has at most two units it shares: the first and the last of its share
-    const bool first = share(total, c, n) / per_unit == unit;
-    return a.part + ((size_t)c * 2 + (first ? 0 : 1)) * slot + warp_at;
-  };
-  float4 *mine = part_of(me);
+  const size_t slot = (size_t)kWarps * 2 * tiles * 32;
+  // a CTA has at most two units it shares: the first of its share, and the last, where that is another one; all but the first
+  // contributor begin inside the unit
+  const int late = share(total, c0, n) / per_unit == unit ? 0 : 1;
+  float4 *const parts = a.part + (size_t)(threadIdx.x >> 5) * 2 * tiles * 32 + (threadIdx.x & 31);
+  float4 *const mine = parts + ((size_t)me * 2 + (me == c0 ? late : 0)) * slot;
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-    if (t < nt) __stcg(mine + t * 32, make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]));
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      if (t < nt) __stcg(mine + (j * tiles + t) * 32, make_float4(acc[j][t][0], acc[j][t][1], acc[j][t][2], acc[j][t][3]));
   __threadfence();
   consumer_barrier();
   if (threadIdx.x == 0) {
@@ -405,67 +425,156 @@ __device__ bool meet_parts(const MoeArgs &a, float (&acc)[NT][4], int nt, int64_
   if (!last) return false;
   __threadfence();
 #pragma unroll
-  for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
-  for (int c = c0; c <= c1; ++c) {
-    const float4 *p = part_of(c);
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
       if (t < nt) {
-        const float4 v = __ldcg(p + t * 32);
-        acc[t][0] += v.x, acc[t][1] += v.y, acc[t][2] += v.z, acc[t][3] += v.w;
+        const float4 *p = parts + (j * tiles + t) * 32;
+        float4 sum = __ldcg(p + ((size_t)c0 * 2 + late) * slot);
+#pragma unroll 8
+        for (int c = c0 + 1; c <= c1; ++c) {
+          const float4 v = __ldcg(p + (size_t)c * 2 * slot);
+          sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+        }
+        acc[j][t][0] = sum.x, acc[j][t][1] = sum.y, acc[j][t][2] = sum.z, acc[j][t][3] = sum.w;
       }
-  }
   return true;
+}
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst), "l"(map),
+               "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+               : "memory");
 }
 
 // ---- first launch ------------------------------------------------------------------------------------------------------
 
 template <int NT>   // row tiles of eight: ceil(M / 8) at most
 __global__ void __launch_bounds__(kThreads, 1)
-moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const MoeArgs a) {
+moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_r,
+              const MoeArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ __align__(8) uint64_t bars[2 * kStages];
   __shared__ int flag;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, P = a.M * a.k;
-  const Routes r(smem, P, a.E);
-  if (tid == 0) init_ring(bars, a.stages);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, P = a.M * a.k, most = most_chosen(P, a.E);
+  const Chosen ch(smem, most, a.M);
+  const Routes r(smem + (Chosen::words(most, a.M) * 4 + 7) / 8 * 8, P, a.E);
+  if (tid == 0) {
+    init_ring(bars, a.stages);
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_w) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_x) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_r) : "memory");
+  }
+  for (int e = tid; e < a.E; e += kThreads) r.mask[e] = make_uint2(0u, 0u);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  cluster_sync();   // the peers are there
-  float *logits = (float *)(smem + a.off_ring), *red = logits + (size_t)a.M * a.E;
-  router_logits(a, logits, red);
-  cluster_sync();
-  if (warp < kWarps)
-    for (int m = warp; m < a.M; m += kWarps) choose(a, logits, r, m);
   __syncthreads();
-  if (blockIdx.x == 0)
+  Ring ring = make_ring(a, smem, bars);
+  const LogitShare mine(a);
+  const int tiles = (a.M + 7) / 8;
+  float *logits = (float *)(smem + a.off_ring);   // [M][256], over the ring once its chunks are used
+  if (warp >= kWarps) {
+    if (lane == 0)
+      for (int c = mine.begin; c < mine.end; ++c) {
+        if (!ring.wait_empty(a)) break;
+        const uint32_t bar = ring.full + 8 * ring.s, st = ring.stage();
+        if (warp > kWarps) {
+          mbar_expect_tx(bar, a.M * 128);
+          tma_load_2d(st + kChunk, &tm_x, bar, c * 64, 0);
+        } else if (a.router_copies) {
+          const int boxes = min(4, (a.E - mine.e0 + 63) / 64);
+          mbar_expect_tx(bar, boxes * kBox);
+          for (int b = 0; b < boxes; ++b) tma_load_2d(st + b * kBox, &tm_r, bar, mine.e0 + b * 64, c * 64);
+        } else {
+          mbar_arrive(bar);
+        }
+        ring.next();
+      }
+    __syncwarp();
+  } else {
+    float acc[2][NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[0][t][e] = acc[1][t][e] = 0.f;
+    const int box = (warp >> 1) * kBox, byte_col = (warp & 1) * 64 + ((lane >> 3) & 1) * 16;
+    for (int ck = mine.begin; ck < mine.end; ++ck) {
+      ring.wait_full(a);
+      const uint32_t st = ring.stage(), xs = st + kChunk;
+      for (int p = 0; p < (a.router_f32 ? 3 : 1); ++p) {
+        if (!a.router_copies) {
+          consumer_barrier();
+          fill_router(a, smem + a.off_ring + ring.s * ring.stage_bytes, mine.e0, ck * 64, p);
+          consumer_barrier();
+        }
+        uint32_t w[2][4][4];
+        load_weights(st + box, byte_col, w[0]);
+        load_weights(st + box, byte_col + 32, w[1]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (t >= tiles) continue;
+          const int m = min(t * 8 + (lane & 7), a.M - 1);
+          product(w, xs + m * 128, (m & 7) << 4, acc, t);
+        }
+      }
+      if (!a.router_copies) fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
+      ring.next();
+    }
+    consumer_barrier();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int m = t * 8 + (lane & 3) * 2 + (e & 1);
+          if (m < a.M) logits[m * kLogitCols + warp * 32 + j * 16 + (lane >> 2) + (e >> 1) * 8] = acc[j][t][e];
+        }
+  }
+  cluster_sync();   // every peer's part is there
+  if (warp < kWarps)
+    for (int m = (int)cluster_rank() + kCluster * warp; m < a.M; m += kCluster * kWarps) choose(a, logits, mine.slices, r, m);
+  fence_async_smem();   // the logits' memory belongs to the copies from here on
+  __syncwarp();
+  cluster_sync();
+  turn_round(r, ch, a.M, a.E, a.k);
+  if (blockIdx.x == 0) {
+    for (int i = tid; i < Chosen::words(most, a.M); i += kThreads) a.table[i] = ((const int *)smem)[i];
     for (int p = tid; p < P; p += kThreads) {
-      a.route_idx[p] = r.idx[p], a.route_w[p] = r.w[p];
       if (a.experts) a.experts[p] = r.idx[p];
       if (a.weights) a.weights[p] = r.w[p];
     }
-  fence_async_smem();   // the logits' memory belongs to the copies from here on
-  turn_round(r, P, a.E, a.k);
+  }
 
-  const int strips = (a.F + 63) / 64, per_unit = (a.D + 63) / 64;
-  const int64_t total = (int64_t)*r.n_act * strips * per_unit;
+  const int strips = (a.F + kUpCols - 1) / kUpCols, per_unit = (a.D + 63) / 64;
+  const int64_t total = (int64_t)*ch.n * strips * per_unit;
   const int n = (int)min((int64_t)gridDim.x, total);
   if ((int)blockIdx.x >= n) return;
   const int64_t begin = share(total, blockIdx.x, n), end = share(total, blockIdx.x + 1, n);
-  Ring ring = make_ring(a, smem, bars);
   int64_t unit = begin / per_unit;
   int chunk = (int)(begin - unit * per_unit);
   int x = (int)(unit / strips), strip = (int)(unit - (int64_t)x * strips);
-  if (warp == kWarps) {
+  if (warp >= kWarps) {
     if (lane == 0)
       for (int64_t i = begin; i < end; ++i) {
         if (!ring.wait_empty(a)) break;
         const uint32_t bar = ring.full + 8 * ring.s, st = ring.stage();
-        mbar_expect_tx(bar, 2 * kBox + a.M * 128);
-        tma_load_3d(st, &tm_w, bar, strip * 64, chunk * 64, r.act[x]);
-        tma_load_3d(st + kBox, &tm_w, bar, a.F + strip * 64, chunk * 64, r.act[x]);
-        tma_load_2d(st + 2 * kBox, &tm_x, bar, chunk * 64, 0);
+        if (warp > kWarps) {
+          mbar_expect_tx(bar, a.M * 128);
+          tma_load_2d(st + kChunk, &tm_x, bar, chunk * 64, 0);
+        } else {
+          mbar_expect_tx(bar, kChunk);
+          const int e = ch.expert[x];
+          if (a.blocks) {
+            tma_load_5d(st, &tm_w, bar, 0, chunk * 64, 0, strip * 2, e);
+          } else {
+            tma_load_4d(st, &tm_w, bar, strip * kUpCols, chunk * 64, 0, e);
+            tma_load_4d(st + 2 * kBox, &tm_w, bar, strip * kUpCols + 64, chunk * 64, 0, e);
+          }
+        }
         ring.next();
         if (++chunk == per_unit) {
           chunk = 0;
@@ -474,65 +583,54 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       }
     return;
   }
+  // a warp has sixteen gate columns and the up columns that go with them, as two tiles of eight and eight
+  const int box = (warp >> 2) * 2 * kBox + ((lane >> 3) & 1) * kBox, byte_col = (warp & 3) * 32;
   for (int64_t i = begin; i < end; ++unit) {
-    const uint2 mask = r.mask[r.act[x]];
+    const uint2 mask = ch.mask[x];
     const int rows = rows_of(mask), nt = (rows + 7) / 8;
-    float acc[NT][4];
+    float acc[2][NT][4];
     int x_row[NT];   // the row of X this lane addresses in each tile
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[0][t][e] = acc[1][t][e] = 0.f;
       x_row[t] = t < nt ? nth_row(mask, min(t * 8 + (lane & 7), rows - 1)) : 0;
     }
     for (; chunk < per_unit && i < end; ++chunk, ++i) {
       ring.wait_full(a);
-      const uint32_t st = ring.stage(), xs = st + 2 * kBox;
-      uint32_t w[4][4];
-      // eight gate columns and the eight up columns that go with them
-      load_weights(st + ((lane >> 3) & 1) * kBox, warp * 16, w);
+      const uint32_t st = ring.stage(), xs = st + kChunk;
+      uint32_t w[2][4][4];
+      load_weights(st + box, byte_col, w[0]);
+      load_weights(st + box, byte_col + 16, w[1]);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         if (t >= nt) continue;
-        const uint32_t at = xs + x_row[t] * 128;
-        const int sw = (x_row[t] & 7) << 4;
-        uint32_t b[4], c[4];
-        ldmatrix4(at + (((lane >> 3) * 16) ^ sw), b);
-        ldmatrix4(at + ((64 + (lane >> 3) * 16) ^ sw), c);
-        float d[4] = {0.f, 0.f, 0.f, 0.f};
-        mma(d, w[0], b[0], b[1]);
-        mma(d, w[1], b[2], b[3]);
-        mma(d, w[2], c[0], c[1]);
-        mma(d, w[3], c[2], c[3]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[t][e] += d[e];
+        product(w, xs + x_row[t] * 128, (x_row[t] & 7) << 4, acc, t);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
       ring.next();
     }
     if (meet_parts<NT>(a, acc, nt, total, n, per_unit, unit, &flag)) {
-      const int col = strip * 64 + warp * 8 + (lane >> 2);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int row = t * 8 + (lane & 3) * 2 + h;
-          if (row >= rows || col >= a.F) continue;
-          const int m = nth_row(mask, row), e = r.act[x];
-          float w = 0.f;
-          for (int j = 0; j < a.k; ++j)
-            if (r.idx[m * a.k + j] == e) w = r.w[m * a.k + j];
-          const float gate = acc[t][h], up = acc[t][2 + h];
-          float v = __fdividef(gate, 1.f + __expf(-gate)) * up * w;
-          __nv_bfloat16 *dst = a.H + (size_t)(r.first[x] + row) * a.F + col;
-          for (int p = 0; p < a.planes; ++p) {
-            const __nv_bfloat16 b = __float2bfloat16_rn(v);
-            dst[(size_t)p * P * a.F] = b;
-            const float back = __bfloat162float(b);
-            v = isfinite(back) ? v - back : 0.f;
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int row = t * 8 + (lane & 3) * 2 + h, col = strip * kUpCols + warp * 16 + j * 8 + (lane >> 2);
+            if (row >= rows || col >= a.ldh) continue;   // (columns from F on come out as zero: their weights are)
+            const int pair = ch.first[x] + row;
+            const float gate = acc[j][t][h], up = acc[j][t][2 + h];
+            float v = __fdividef(gate, 1.f + __expf(-gate)) * up * r.pair_w[pair];
+            __nv_bfloat16 *dst = a.H + (size_t)pair * a.ldh + col;
+            for (int p = 0; p < a.planes; ++p) {
+              const __nv_bfloat16 b = __float2bfloat16_rn(v);
+              dst[(size_t)p * P * a.ldh] = b;
+              const float back = __bfloat162float(b);
+              v = isfinite(back) ? v - back : 0.f;
+            }
           }
-        }
-      }
     }
     chunk = 0;
     if (++strip == strips) strip = 0, ++x;
@@ -548,91 +646,107 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ __align__(8) uint64_t bars[2 * kStages];
   __shared__ int flag;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, P = a.M * a.k;
-  const Routes r(smem, P, a.E);
-  if (tid == 0) init_ring(bars, a.stages);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, P = a.M * a.k, most = most_chosen(P, a.E);
+  const Chosen ch(smem, most, a.M);
+  if (tid == 0) {
+    init_ring(bars, a.stages);
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_w) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_h) : "memory");
+  }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int p = tid; p < P; p += kThreads) r.idx[p] = a.route_idx[p], r.w[p] = a.route_w[p];
+  for (int i = tid; i < Chosen::words(most, a.M); i += kThreads) ((int *)smem)[i] = a.table[i];
   __syncthreads();
-  turn_round(r, P, a.E, a.k);
-  const int n_act = *r.n_act;
-  const int strips = (a.D + 127) / 128, per_expert = (a.F + 63) / 64, per_unit = n_act * per_expert;
+  const int chosen = *ch.n;
+  const int strips = (a.D + kDownCols - 1) / kDownCols, per_expert = (a.F + 63) / 64, per_unit = chosen * per_expert;
   const int tiles = (a.M + 7) / 8;
   const int64_t total = (int64_t)strips * per_unit;
   const int n = (int)min((int64_t)gridDim.x, total);
-  Ring ring = make_ring(a, smem, bars);
-  // what the places without an expert add to a row: nothing, or NaN
-  auto rest = [&](int m) {
-    float s = 0.f;
-    for (int j = 0; j < a.k; ++j)
-      if (r.idx[m * a.k + j] < 0) s += r.w[m * a.k + j];
-    return s;
-  };
   auto put = [&](int m, int c, float v) {
     if (a.y_f32) ((float *)a.Y)[(int64_t)m * a.ldy + c] = v;
     else ((__nv_bfloat16 *)a.Y)[(int64_t)m * a.ldy + c] = __float2bfloat16_rn(v);
   };
   if (total == 0) {   // nobody takes an expert
-    for (int i = blockIdx.x * kThreads + tid; i < a.M * a.D; i += gridDim.x * kThreads) put(i / a.D, i % a.D, rest(i / a.D));
+    for (int i = blockIdx.x * kThreads + tid; i < a.M * a.D; i += gridDim.x * kThreads) put(i / a.D, i % a.D, ch.rest[i / a.D]);
     return;
   }
   if ((int)blockIdx.x >= n) return;
   const int64_t begin = share(total, blockIdx.x, n), end = share(total, blockIdx.x + 1, n);
+  Ring ring = make_ring(a, smem, bars);
   int64_t unit = begin / per_unit;
-  int at = (int)(begin - unit * per_unit), x = at / per_expert, chunk = at - x * per_expert;
-  const int plane_bytes = tiles * 1024;
-  if (warp == kWarps) {
+  const int at = (int)(begin - unit * per_unit);
+  int x = at / per_expert, chunk = at - x * per_expert;
+  const int group_bytes = a.planes * 1024;   // eight hidden rows
+  if (warp >= kWarps) {
     if (lane == 0)
       for (int64_t i = begin; i < end; ++i) {
         if (!ring.wait_empty(a)) break;
         const uint32_t bar = ring.full + 8 * ring.s, st = ring.stage();
-        const int strip = (int)unit, p0 = r.first[x], boxes = (r.first[x + 1] - p0 + 7) / 8;
-        mbar_expect_tx(bar, 2 * kBox + a.planes * boxes * 1024);
-        tma_load_3d(st, &tm_w, bar, strip * 128, chunk * 64, r.act[x]);
-        tma_load_3d(st + kBox, &tm_w, bar, strip * 128 + 64, chunk * 64, r.act[x]);
-        for (int p = 0; p < a.planes; ++p)
-          for (int b = 0; b < boxes; ++b)
-            tma_load_3d(st + 2 * kBox + p * plane_bytes + b * 1024, &tm_h, bar, chunk * 64, p0 + b * 8, p);
+        if (warp > kWarps) {
+          const int p0 = ch.first[x], groups = (ch.first[x + 1] - p0 + 7) / 8;
+          mbar_expect_tx(bar, groups * group_bytes);
+          for (int g = 0; g < groups; ++g) tma_load_3d(st + kChunk + g * group_bytes, &tm_h, bar, chunk * 64, p0 + g * 8, 0);
+        } else {
+          mbar_expect_tx(bar, kChunk);
+          const int e = ch.expert[x];
+          if (a.blocks) {
+            tma_load_4d(st, &tm_w, bar, 0, chunk * 64, (int)unit * 4, e);
+          } else {
+            for (int b = 0; b < 4; ++b) tma_load_3d(st + b * kBox, &tm_w, bar, (int)unit * kDownCols + b * 64, chunk * 64, e);
+          }
+        }
         ring.next();
         if (++chunk == per_expert) {
           chunk = 0;
-          if (++x == n_act) x = 0, ++unit;
+          if (++x == chosen) x = 0, ++unit;
         }
       }
     return;
   }
+  // a warp has 32 columns, as two tiles of sixteen
+  const int box = (warp >> 1) * kBox, byte_col = (warp & 1) * 64 + ((lane >> 3) & 1) * 16;
   for (int64_t i = begin; i < end; ++unit) {
-    float acc[NT][4];
+    float acc[2][NT][4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
-    for (; x < n_act && i < end; ++x, chunk = 0) {
-      const uint2 mask = r.mask[r.act[x]];
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[0][t][e] = acc[1][t][e] = 0.f;
+    for (; x < chosen && i < end; ++x, chunk = 0) {
+      const uint2 mask = ch.mask[x];
       for (; chunk < per_expert && i < end; ++chunk, ++i) {
         ring.wait_full(a);
-        const uint32_t st = ring.stage(), hs = st + 2 * kBox;
-        uint32_t w[4][4];
-        load_weights(st + (warp >> 2) * kBox, (warp & 3) * 32 + ((lane >> 3) & 1) * 16, w);
+        const uint32_t st = ring.stage(), hs = st + kChunk;
+        uint32_t w[2][4][4];
+        load_weights(st + box, byte_col, w[0]);
+        load_weights(st + box, byte_col + 32, w[1]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const uint32_t here = (t < 4 ? mask.x : mask.y) >> (8 * (t & 3)) & 255u;   // rows of the tile that take the expert
           if (!here) continue;
           const int m = t * 8 + (lane & 7), row = takes(mask, m) ? rows_below(mask, m) : 0;
-          float d[4] = {0.f, 0.f, 0.f, 0.f};
+          const uint32_t h = hs + (row >> 3) * group_bytes + (row & 7) * 128;
+          const int sw = (row & 7) << 4;
+          float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
           for (int p = 0; p < a.planes; ++p) {
-            const uint32_t h = hs + p * plane_bytes + row * 128;
-            const int sw = (row & 7) << 4;
             uint32_t b[4], c[4];
-            ldmatrix4(h + (((lane >> 3) * 16) ^ sw), b);
-            ldmatrix4(h + ((64 + (lane >> 3) * 16) ^ sw), c);
-            mma(d, w[0], b[0], b[1]);
-            mma(d, w[1], b[2], b[3]);
-            mma(d, w[2], c[0], c[1]);
-            mma(d, w[3], c[2], c[3]);
+            ldmatrix4(h + p * 1024 + (((lane >> 3) * 16) ^ sw), b);
+            ldmatrix4(h + p * 1024 + ((64 + (lane >> 3) * 16) ^ sw), c);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) mma(d[j], w[j][0], b[0], b[1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) mma(d[j], w[j][1], b[2], b[3]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) mma(d[j], w[j][2], c[0], c[1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) mma(d[j], w[j][3], c[2], c[3]);
           }
           // (the other rows' columns hold whatever the stage did)
-          if (here >> (2 * (lane & 3)) & 1u) acc[t][0] += d[0], acc[t][2] += d[2];
-          if (here >> (2 * (lane & 3) + 1) & 1u) acc[t][1] += d[1], acc[t][3] += d[3];
+          const bool k0 = here >> (2 * (lane & 3)) & 1u, k1 = here >> (2 * (lane & 3) + 1) & 1u;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if (k0) acc[j][t][0] += d[j][0], acc[j][t][2] += d[j][2];
+            if (k1) acc[j][t][1] += d[j][1], acc[j][t][3] += d[j][3];
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
@@ -642,14 +756,15 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     }
     x = 0, chunk = 0;
     if (meet_parts<NT>(a, acc, tiles, total, n, per_unit, unit, &flag)) {
-      const int col = (int)unit * 128 + warp * 16 + (lane >> 2);
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int m = t * 8 + (lane & 3) * 2 + (e & 1), c = col + (e >> 1) * 8;
-          if (m < a.M && c < a.D) put(m, c, acc[t][e] + rest(m));
-        }
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int m = t * 8 + (lane & 3) * 2 + (e & 1), c = (int)unit * kDownCols + warp * 32 + j * 16 + (lane >> 2) + (e >> 1) * 8;
+            if (m < a.M && c < a.D) put(m, c, acc[j][t][e] + ch.rest[m]);
+          }
     }
   }
 }
@@ -659,42 +774,44 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 int row_tiles(int64_t M) { return (int)((M + 7) / 8); }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
+int hidden_pitch(int F) { return (F + 63) / 64 * 64; }
 struct MoeLayout {
-  size_t idx, w, h, part, total;
+  size_t table, h, part, total;
 };
 MoeLayout moe_layout(const alg_moe_s &h, int64_t M) {
   MoeLayout L;
   const size_t P = (size_t)M * h.k;
   size_t off = 0;
-  L.idx = off, off = up256(off + P * 4);
-  L.w = off, off = up256(off + P * 4);
-  L.h = off, off = up256(off + 3 * P * h.F * 2);
-  L.part = off, off = up256(off + (size_t)h.num_sms * 2 * kWarps * row_tiles(M) * 512);
+  L.table = off, off = up256(off + (size_t)Chosen::words(most_chosen((int)P, h.E), (int)M) * 4);
+  L.h = off, off = up256(off + 3 * P * hidden_pitch(h.F) * 2);
+  L.part = off, off = up256(off + (size_t)h.num_sms * 2 * kWarps * 2 * row_tiles(M) * 512);
   L.total = off;
   return L;
 }
 
-using MoeKernel = void (*)(const CUtensorMap, const CUtensorMap, const MoeArgs);
-MoeKernel up_kernel(int tiles) {
+using UpKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const MoeArgs);
+using DownKernel = void (*)(const CUtensorMap, const CUtensorMap, const MoeArgs);
+UpKernel up_kernel(int tiles) {
   return tiles <= 1 ? moe_up_kernel<1> : tiles <= 2 ? moe_up_kernel<2> : tiles <= 4 ? moe_up_kernel<4> : moe_up_kernel<8>;
 }
-MoeKernel down_kernel(int tiles) {
+DownKernel down_kernel(int tiles) {
   return tiles <= 1 ? moe_down_kernel<1> : tiles <= 2 ? moe_down_kernel<2> : tiles <= 4 ? moe_down_kernel<4> : moe_down_kernel<8>;
 }
 cudaError_t moe_attributes() {
   static OncePerDevice once;
   return once([] {
     for (int t : {1, 2, 4, 8})
-      for (MoeKernel k : {up_kernel(t), down_kernel(t)}) {
-        const cudaError_t e = cudaFuncSetAttribute((const void *)k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+      for (const void *k : {(const void *)up_kernel(t), (const void *)down_kernel(t)}) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
         if (e != cudaSuccess) return e;
       }
     return cudaSuccess;
   });
 }
-// Ring behind the routes: as many stages as fit.
-bool fit_ring(MoeArgs &a, int stage_bytes, size_t scratch, size_t *smem) {
-  a.off_ring = (int)((Routes::bytes(a.M * a.k, a.E) + 1023) / 1024 * 1024);
+// Ring behind the tables: as many stages as fit.
+bool fit_ring(MoeArgs &a, bool routes, int stage_bytes, size_t scratch, size_t *smem) {
+  const int P = a.M * a.k, table = (Chosen::words(most_chosen(P, a.E), a.M) * 4 + 7) / 8 * 8;
+  a.off_ring = (int)((table + (routes ? Routes::bytes(P, a.E) : 0) + 1023) / 1024 * 1024);
   a.stage_bytes = stage_bytes;
   a.stages = (kSmemLimit - 1024 - a.off_ring) / stage_bytes;
   if (a.stages > kStages) a.stages = kStages;
@@ -704,8 +821,8 @@ bool fit_ring(MoeArgs &a, int stage_bytes, size_t scratch, size_t *smem) {
   return a.stages >= 2 && *smem <= (size_t)kSmemLimit;
 }
 
-cudaError_t launch_moe(MoeKernel k, const CUtensorMap &tm_w, const CUtensorMap &tm_b, const MoeArgs &a, int grid, int cluster, size_t smem,
-                       cudaStream_t st) {
+template <typename... Params>
+cudaError_t launch_moe(void (*k)(Params...), int grid, int cluster, size_t smem, cudaStream_t st, Params... params) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(kThreads);
@@ -718,7 +835,7 @@ cudaError_t launch_moe(MoeKernel k, const CUtensorMap &tm_w, const CUtensorMap &
   at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k, tm_w, tm_b, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k, params...);
   if (e == cudaSuccess) count_launch(1);
   return e;
 }
@@ -811,37 +928,57 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   a.sigmoid = h->score == ALG_MOE_SIGMOID, a.renormalise = h->renormalise, a.route_scale = h->route_scale;
   a.y_f32 = y_dtype == ALG_F32, a.planes = a.y_f32 ? 3 : 2;
   a.X = (const __nv_bfloat16 *)X, a.ldx = ldx;
-  a.W_router = W_router, a.router_f32 = h->router_dtype == ALG_F32, a.router_vec = h->E % 8 == 0 && on_16(W_router, h->E, er);
+  a.W_router = W_router, a.router_f32 = h->router_dtype == ALG_F32, a.router_copies = !a.router_f32 && on_16(W_router, h->E, er);
   a.bias = select_bias, a.experts = experts, a.weights = weights;
   a.Y = Y, a.ldy = ldy;
-  a.route_idx = (int *)(ws + L.idx), a.route_w = (float *)(ws + L.w);
-  a.H = (__nv_bfloat16 *)(ws + L.h), a.part = (float4 *)(ws + L.part);
+  a.table = (int *)(ws + L.table), a.H = (__nv_bfloat16 *)(ws + L.h), a.ldh = hidden_pitch(h->F), a.part = (float4 *)(ws + L.part);
   a.status = h->d_state, a.wait_limit = kDefaultWaitLimit;
 
   const int tiles = row_tiles(M);
   CUtensorMap tm_up, tm_x, tm_down, tm_h;
-  {
-    const uint64_t d[3] = {(uint64_t)2 * h->F, (uint64_t)h->D, (uint64_t)h->E}, s[2] = {(uint64_t)4 * h->F, (uint64_t)4 * bank};
-    const uint32_t b[3] = {64, 64, 1};
-    if (make_map_nd(&tm_up, W_gate_up, 3, d, s, b, 128) != cudaSuccess) return ALG_ERR_CUDA;
-    const uint64_t dd[3] = {(uint64_t)h->D, (uint64_t)h->F, (uint64_t)h->E}, sd[2] = {(uint64_t)2 * h->D, (uint64_t)2 * bank};
-    if (make_map_nd(&tm_down, W_down, 3, dd, sd, b, 128) != cudaSuccess) return ALG_ERR_CUDA;
-    const uint64_t dx[2] = {(uint64_t)h->D, (uint64_t)M}, sx[1] = {(uint64_t)ldx * 2};
-    const uint32_t bx[2] = {64, (uint32_t)M};
-    if (make_map_nd(&tm_x, X, 2, dx, sx, bx, 128) != cudaSuccess) return ALG_ERR_CUDA;
-    const uint64_t dh[3] = {(uint64_t)h->F, (uint64_t)P, 3}, sh[2] = {(uint64_t)2 * h->F, (uint64_t)2 * P * h->F};
-    const uint32_t bh[3] = {64, 8, 1};
-    if (make_map_nd(&tm_h, a.H, 3, dh, sh, bh, 128) != cudaSuccess) return ALG_ERR_CUDA;
+  const uint64_t D = h->D, F = h->F, E = h->E, H = a.ldh, up_row = 4 * F, down_row = 2 * D;
+  cudaError_t e;
+  if (F % 64 == 0) {   // {column of a block, row, gate / up, column block, expert}
+    const uint64_t d[5] = {64, D, 2, F / 64, E}, s[4] = {up_row, 2 * F, 128, up_row * D};
+    const uint32_t b[5] = {64, 64, 2, 2, 1};
+    e = make_map_nd(&tm_up, W_gate_up, 5, d, s, b, 128);
+  } else {             // {column, row, gate / up, expert}: what is past F reads as zero
+    const uint64_t d[4] = {F, D, 2, E}, s[3] = {up_row, 2 * F, up_row * D};
+    const uint32_t b[4] = {64, 64, 2, 1};
+    e = make_map_nd(&tm_up, W_gate_up, 4, d, s, b, 128);
   }
+  if (e != cudaSuccess) return ALG_ERR_CUDA;
+  if (D % 64 == 0) {   // {column of a block, row, column block, expert}
+    const uint64_t d[4] = {64, F, D / 64, E}, s[3] = {down_row, 128, down_row * F};
+    const uint32_t b[4] = {64, 64, 4, 1};
+    e = make_map_nd(&tm_down, W_down, 4, d, s, b, 128);
+  } else {
+    const uint64_t d[3] = {D, F, E}, s[2] = {down_row, down_row * F};
+    const uint32_t b[3] = {64, 64, 1};
+    e = make_map_nd(&tm_down, W_down, 3, d, s, b, 128);
+  }
+  if (e != cudaSuccess) return ALG_ERR_CUDA;
+  const uint64_t dx[2] = {D, (uint64_t)M}, sx[1] = {(uint64_t)ldx * 2};
+  const uint32_t bx[2] = {64, (uint32_t)M};
+  const uint64_t dh[3] = {H, (uint64_t)P, 3}, sh[2] = {2 * H, 2 * P * H};
+  const uint32_t bh[3] = {64, 8, (uint32_t)a.planes};
+  if (make_map_nd(&tm_x, X, 2, dx, sx, bx, 128) != cudaSuccess || make_map_nd(&tm_h, a.H, 3, dh, sh, bh, 128) != cudaSuccess) return ALG_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   size_t smem = 0;
-  const int per = ((h->E + kCluster - 1) / kCluster + 7) / 8 * 8;
-  if (!fit_ring(a, 2 * kBox + tiles * 1024, ((size_t)M * h->E + (size_t)kWarps * kRouterRows * per) * 4, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
+  CUtensorMap tm_r = tm_x;
+  if (a.router_copies) {
+    const uint64_t dr[2] = {E, D}, sr[1] = {2 * E};
+    const uint32_t br[2] = {64, 64};
+    if (make_map_nd(&tm_r, W_router, 2, dr, sr, br, 128) != cudaSuccess) return ALG_ERR_CUDA;
+  }
+  a.blocks = F % 64 == 0;
+  if (!fit_ring(a, true, kChunk + tiles * 1024, (size_t)M * kLogitCols * 4, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
   a.count = h->d_state + 4;
-  if (launch_moe(up_kernel(tiles), tm_up, tm_x, a, h->clusters * kCluster, kCluster, smem, st) != cudaSuccess) return ALG_ERR_CUDA;
-  if (!fit_ring(a, 2 * kBox + a.planes * tiles * 1024, 0, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
+  if (launch_moe(up_kernel(tiles), h->clusters * kCluster, kCluster, smem, st, tm_up, tm_x, tm_r, a) != cudaSuccess) return ALG_ERR_CUDA;
+  a.blocks = D % 64 == 0;
+  if (!fit_ring(a, false, kChunk + a.planes * tiles * 1024, 0, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
   a.count = h->d_state + 4 + h->num_sms;
-  return launch_moe(down_kernel(tiles), tm_down, tm_h, a, h->num_sms, 1, smem, st) == cudaSuccess ? ALG_OK : ALG_ERR_CUDA;
+  return launch_moe(down_kernel(tiles), h->num_sms, 1, smem, st, tm_down, tm_h, a) == cudaSuccess ? ALG_OK : ALG_ERR_CUDA;
 }
 
 alg_status_t alg_moe_last_status(alg_moe_t h, void *stream, alg_status_t *status) {
