@@ -52,6 +52,7 @@ constexpr int kStages = 6;                  // at most
 constexpr int kBox = 64 * 64 * 2;           // 64 columns of 64 rows of weights
 constexpr int kChunk = 4 * kBox;            // up: [column block][gate, up]; down: [column block]
 constexpr int kUpCols = 128, kDownCols = 256;
+constexpr int kAhead = 12;                  // chunks of a share of the second launch that the first asks into L2
 constexpr int kSmemLimit = 225 * 1024;
 constexpr int kMaxM = ALG_MOE_MAX_M;
 constexpr int kLogitCols = 256;             // experts a CTA has logits of
@@ -72,6 +73,7 @@ struct MoeArgs {
   __nv_bfloat16 *H;           // workspace: weighted hidden rows, [planes][M * k][ldh]
   int ldh;                    // F to the next multiple of 64
   float4 *part;               // workspace: partial sums, [CTA][2][8 warps][2][row tiles][32 lanes]
+  int down_ctas, down_blocks; // of the second launch
   int blocks;                 // tensor maps of whole column blocks (one copy a chunk)
   int *count;                 // [CTA]: arrivals at the unit whose first contributor it is
   int *status;
@@ -126,18 +128,13 @@ __device__ __forceinline__ int nth_row(uint2 m, int n) {   // n < rows_of(m)
   return __ffs(w) - 1 + (n < lo ? 0 : 32);
 }
 
-// From r.idx and r.w, with r.mask zero; all threads of the CTA.
+__device__ __forceinline__ void consumer_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory"); }
+// From r.idx, with r.mask zero; all threads of the CTA.
 __device__ void turn_round(const Routes &r, const Chosen &ch, int M, int E, int k) {
   const int tid = threadIdx.x, P = M * k;
   for (int p = tid; p < P; p += kThreads) {
     const int e = r.idx[p], m = p / k;
     if (e >= 0) atomicOr(m < 32 ? &r.mask[e].x : &r.mask[e].y, 1u << (m & 31));
-  }
-  for (int m = tid; m < M; m += kThreads) {
-    float s = 0.f;
-    for (int j = 0; j < k; ++j)
-      if (r.idx[m * k + j] < 0) s += r.w[m * k + j];
-    ch.rest[m] = s;
   }
   __syncthreads();
   if (tid < 32) {
@@ -161,14 +158,22 @@ __device__ void turn_round(const Routes &r, const Chosen &ch, int M, int E, int 
     if (tid == 0) ch.first[n] = pairs, *ch.n = n;
   }
   __syncthreads();
-  for (int p = tid; p < P; p += kThreads) {
+}
+// What only the consumers need, by them.
+__device__ void weigh_pairs(const Routes &r, const Chosen &ch, int M, int k) {
+  for (int p = threadIdx.x; p < M * k; p += kConsumers) {
     const int e = r.idx[p], m = p / k;
     if (e >= 0) r.pair_w[ch.first[r.place[e]] + rows_below(r.mask[e], m)] = r.w[p];
   }
-  __syncthreads();
+  for (int m = threadIdx.x; m < M; m += kConsumers) {
+    float s = 0.f;
+    for (int j = 0; j < k; ++j)
+      if (r.idx[m * k + j] < 0) s += r.w[m * k + j];
+    ch.rest[m] = s;
+  }
+  consumer_barrier();
 }
 
-__device__ __forceinline__ void consumer_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory"); }
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -213,76 +218,80 @@ __device__ void fill_router(const MoeArgs &a, uint8_t *stage, int e0, int k0, in
   }
 }
 
-// A warp adds up the logits of row m and chooses its experts, for all CTAs of the cluster.  Without a bias the order is that of the
-// logits, which a score that underflows or saturates cannot spoil.
-__device__ void choose(const MoeArgs &a, const float *logits, int slices, const Routes &r, int m) {
-  constexpr int kMost = ALG_MOE_MAX_EXPERTS / 32;
-  const int lane = threadIdx.x & 31;
-  float l[kMost], key[kMost];
-  bool bad = false;
-  float top = -FLT_MAX;
-#pragma unroll
-  for (int i = 0; i < kMost; ++i) {
-    l[i] = 0.f;
-    key[i] = -INFINITY;
-    if (32 * i >= a.E) continue;
-    const int e = min(lane + 32 * i, a.E - 1), first = e / kLogitCols * slices;
-    const uint32_t at = smem_u32(logits + m * kLogitCols + (e & (kLogitCols - 1)));
-    float part[kCluster];
+// The logits of rows rank, rank + 8, ...: the peers' parts in their order, to sums[row / 8][E].
+__device__ void gather_logits(const MoeArgs &a, const float *parts, int slices, float *sums) {
+  const int rank = (int)cluster_rank();
+  for (int i = threadIdx.x; i < (a.M - rank + kCluster - 1) / kCluster * a.E; i += kConsumers) {
+    const int row = i / a.E, e = i - row * a.E, first = e / kLogitCols * slices;
+    const uint32_t at = smem_u32(parts + (rank + kCluster * row) * kLogitCols + (e & (kLogitCols - 1)));
+    float part[kCluster], sum = 0.f;
 #pragma unroll
     for (int p = 0; p < kCluster; ++p) {
       uint32_t there;
       part[p] = 0.f;
       if (p < slices) {
         asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(first + p));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[p]) : "r"(there) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[p]) : "r"(there));
       }
     }
 #pragma unroll
-    for (int p = 0; p < kCluster; ++p) l[i] += part[p];
-    bad = bad || !isfinite(l[i]);
-    top = fmaxf(top, l[i]);
+    for (int p = 0; p < kCluster; ++p) sum += part[p];
+    sums[i] = sum;
   }
-  bad = __any_sync(~0u, bad);
+}
+
+// The experts of this CTA's rows (rank, rank + 8, ...: eight at most, one a warp), for all CTAs of the cluster.  An expert's place is
+// the number of experts in front of it.  Without a bias the order is that of the logits, which a score that underflows or saturates
+// cannot spoil.  Short loops on purpose: this code runs once a launch and costs what its instructions take to arrive.  All consumers.
+__device__ void choose(const MoeArgs &a, const float *logits, uint8_t *scratch, const Routes &r) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pitch = (a.E + 3) & ~3;
+  const int rank = (int)cluster_rank(), rows = (a.M - rank + kCluster - 1) / kCluster;
+  float *keys = (float *)scratch, *top_of = keys + 8 * pitch, *sum_of = top_of + 8;
+  int *place = (int *)(sum_of + 8);   // [8][k]
+  const int m = rank + kCluster * warp;
+  const float *l = logits + warp * a.E;
+  auto score = [&](float x, float top, float sum) { return a.sigmoid ? 1.f / (1.f + expf(-x)) : expf(x - top) / sum; };
+  bool bad = false;
+  float top = -FLT_MAX, sum = 1.f;
+  if (warp < rows) {
+#pragma unroll 4
+    for (int e = lane; e < a.E; e += 32) bad = bad || !isfinite(l[e]), top = fmaxf(top, l[e]);
+    bad = __any_sync(~0u, bad);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-  float sum = 1.f;
-  if (!a.sigmoid && (a.bias || !a.renormalise)) {   // (else the sum cancels)
-    sum = 0.f;
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if (!a.sigmoid && (a.bias || !a.renormalise)) {   // (else the sum cancels)
+      sum = 0.f;
+#pragma unroll 1
+      for (int e = lane; e < a.E; e += 32) sum += expf(l[e] - top);
 #pragma unroll
-    for (int i = 0; i < kMost; ++i)
-      if (lane + 32 * i < a.E) sum += expf(l[i] - top);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-  }
-  auto score = [&](float x) { return a.sigmoid ? 1.f / (1.f + expf(-x)) : expf(x - top) / sum; };
-#pragma unroll
-  for (int i = 0; i < kMost; ++i) {
-    const int e = lane + 32 * i;
-    if (e < a.E) {
-      key[i] = a.bias ? score(l[i]) + a.bias[e] : l[i];
-      key[i] = key[i] == key[i] ? key[i] + 0.f : -INFINITY;   // (-0 is 0)
+      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     }
+#pragma unroll 1
+    for (int e = lane; e < pitch; e += 32) {
+      float key = -INFINITY;
+      if (e < a.E && !bad) key = a.bias ? score(l[e], top, sum) + a.bias[e] : l[e];
+      keys[warp * pitch + e] = key == key ? key : -INFINITY;
+    }
+    if (lane < a.k) place[warp * a.k + lane] = -1;
   }
-  int mine = -1;      // lane j keeps the j-th choice
-  float w = 0.f, mine_l = 0.f;
-  for (int j = 0; j < a.k && !bad; ++j) {
-    float best = -INFINITY, at = 0.f;
-    int e = 0x7FFFFFFF;
-#pragma unroll
-    for (int i = 0; i < kMost; ++i)
-      if (32 * i < a.E && key[i] > best) best = key[i], e = lane + 32 * i, at = l[i];
-    const uint32_t bits = __float_as_uint(best), order = bits >> 31 ? ~bits : bits | 0x80000000u;
-    const uint32_t most = __reduce_max_sync(~0u, order);
-    const int win = (int)__reduce_min_sync(~0u, order == most ? (uint32_t)e : 0x7FFFFFFFu);
-    if (win == 0x7FFFFFFF) break;   // nothing left to choose
-    at = __shfl_sync(~0u, at, win & 31);
-#pragma unroll
-    for (int i = 0; i < kMost; ++i)
-      if (lane + 32 * i == win) key[i] = -INFINITY;
-    if (lane == j) mine = win, mine_l = at;
+  consumer_barrier();
+#pragma unroll 1
+  for (int i = threadIdx.x; i < rows * a.E; i += kConsumers) {
+    const int row = i / a.E, e = i - row * a.E;
+    const float *key = keys + row * pitch, mine = key[e];
+    int before = 0;
+#pragma unroll 2
+    for (int f = 0; f < pitch; f += 4) {
+      const float4 v = *(const float4 *)(key + f);
+      before += (v.x > mine || (v.x == mine && f < e)) + (v.y > mine || (v.y == mine && f + 1 < e)) + (v.z > mine || (v.z == mine && f + 2 < e)) +
+                (v.w > mine || (v.w == mine && f + 3 < e));
+    }
+    if (before < a.k && mine > -INFINITY) place[row * a.k + before] = e;
   }
-  if (mine >= 0) w = score(mine_l);
+  consumer_barrier();
+  if (warp >= rows) return;
+  const int mine = lane < a.k ? place[warp * a.k + lane] : -1;
+  float w = mine >= 0 ? score(l[mine], top, sum) : 0.f;
   if (a.renormalise) {
     float s = w;
 #pragma unroll
@@ -301,6 +310,10 @@ __device__ void choose(const MoeArgs &a, const float *logits, int slices, const 
       asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(w) : "memory");
     }
   }
+}
+size_t choose_bytes(int M, int E, int k) {   // logits, their sums, what `choose` works in
+  const size_t rows = (M + kCluster - 1) / kCluster;
+  return ((size_t)M * kLogitCols + rows * E + 3) / 4 * 16 + ((size_t)8 * ((E + 3) & ~3) + 16 + 8 * (size_t)k) * 4;
 }
 
 // ---- the ring ----------------------------------------------------------------------------------------------------------
@@ -390,6 +403,14 @@ __device__ __forceinline__ void product(const uint32_t (&w)[2][4][4], uint32_t a
     for (int e = 0; e < 4; ++e) acc[j][t][e] += d[j][e];
 }
 
+// CTAs that take part: at most one for each chunk, and where there are fewer units than CTAs a whole number for each unit, if that
+// leaves three quarters of them: then a CTA has parts of one unit, not of two, and meets others once.
+__device__ __forceinline__ int takers(int64_t units, int per_unit, int ctas) {
+  if (units * per_unit < ctas) return (int)(units * per_unit);
+  if (units > ctas) return ctas;
+  const int even = ctas / (int)units * (int)units;
+  return 4 * even >= 3 * ctas ? even : ctas;
+}
 // The share of CTA c of n among `total` chunks, and whose share a chunk is in; n <= total, so that nobody's is empty (CTAs past n have none).
 __device__ __forceinline__ int64_t share(int64_t total, int c, int n) { return total * c / n; }
 __device__ __forceinline__ int owner(int64_t total, int64_t chunk, int n) { return (int)(((chunk + 1) * n - 1) / total); }
@@ -412,18 +433,16 @@ __device__ bool meet_parts(const MoeArgs &a, float (&acc)[2][NT][4], int nt, int
 #pragma unroll
     for (int t = 0; t < NT; ++t)
       if (t < nt) __stcg(mine + (j * tiles + t) * 32, make_float4(acc[j][t][0], acc[j][t][1], acc[j][t][2], acc[j][t][3]));
-  __threadfence();
   consumer_barrier();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0) {   // (what the barrier orders before its fence, the fence orders before its count)
+    __threadfence();
     const bool last = atomicAdd(a.count + c0, 1) == c1 - c0;
     if (last) a.count[c0] = 0;   // as the next launch finds it
+    __threadfence();
     *flag = last;
   }
   consumer_barrier();
-  const bool last = *flag;
-  consumer_barrier();
-  if (!last) return false;
-  __threadfence();
+  if (!*flag) return false;   // (nobody writes it again before the barrier of another unit)
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -449,10 +468,26 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map
 
 // ---- first launch ------------------------------------------------------------------------------------------------------
 
+// The first chunks of every share of the second launch are asked into L2, so that HBM does not idle between the launches.
+__device__ void ask_ahead(const CUtensorMap &tm_d, const MoeArgs &a, const Chosen &ch) {
+  const int per_expert = (a.F + 63) / 64, chosen = *ch.n, per_unit = chosen * per_expert;
+  const int strips = (a.D + kDownCols - 1) / kDownCols, n = takers(strips, per_unit, a.down_ctas);
+  const int64_t total = (int64_t)strips * per_unit;
+  for (int c = blockIdx.x; c < n; c += gridDim.x) {
+    const int64_t begin = share(total, c, n), end = min(share(total, c + 1, n), begin + kAhead);
+    for (int64_t i = begin; i < end; ++i) {
+      const int unit = (int)(i / per_unit), at = (int)(i - (int64_t)unit * per_unit), x = at / per_expert;
+      if (a.down_blocks)
+        asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(&tm_d), "r"(0), "r"((at - x * per_expert) * 64),
+                     "r"(unit * 4), "r"(ch.expert[x]));
+    }
+  }
+}
+
 template <int NT>   // row tiles of eight: ceil(M / 8) at most
 __global__ void __launch_bounds__(kThreads, 1)
 moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_r,
-              const MoeArgs a) {
+              const __grid_constant__ CUtensorMap tm_d, const MoeArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ __align__(8) uint64_t bars[2 * kStages];
@@ -467,6 +502,10 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_r) : "memory");
   }
   for (int e = tid; e < a.E; e += kThreads) r.mask[e] = make_uint2(0u, 0u);
+  // the router is asked into L2 while the previous kernel still runs (L2 is where its writes would go: no stale copy)
+  const size_t router = (size_t)a.D * a.E * (a.router_f32 ? 4 : 2);
+  for (size_t i = ((size_t)blockIdx.x * kThreads + tid) * 128; i < router; i += (size_t)gridDim.x * kThreads * 128)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"((const uint8_t *)a.W_router + i));
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
@@ -535,23 +574,30 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
         }
   }
   cluster_sync();   // every peer's part is there
-  if (warp < kWarps)
-    for (int m = (int)cluster_rank() + kCluster * warp; m < a.M; m += kCluster * kWarps) choose(a, logits, mine.slices, r, m);
+  if (warp < kWarps) {
+    float *sums = logits + a.M * kLogitCols;
+    gather_logits(a, logits, mine.slices, sums);
+    consumer_barrier();
+    choose(a, sums, (uint8_t *)logits + (a.M * kLogitCols + (a.M + kCluster - 1) / kCluster * a.E + 3) / 4 * 16, r);
+  }
   fence_async_smem();   // the logits' memory belongs to the copies from here on
   __syncwarp();
   cluster_sync();
   turn_round(r, ch, a.M, a.E, a.k);
-  if (blockIdx.x == 0) {
-    for (int i = tid; i < Chosen::words(most, a.M); i += kThreads) a.table[i] = ((const int *)smem)[i];
-    for (int p = tid; p < P; p += kThreads) {
-      if (a.experts) a.experts[p] = r.idx[p];
-      if (a.weights) a.weights[p] = r.w[p];
+  if (warp < kWarps) {
+    weigh_pairs(r, ch, a.M, a.k);
+    if (blockIdx.x == 0) {
+      for (int i = tid; i < Chosen::words(most, a.M); i += kConsumers) a.table[i] = ((const int *)smem)[i];
+      for (int p = tid; p < P; p += kConsumers) {
+        if (a.experts) a.experts[p] = r.idx[p];
+        if (a.weights) a.weights[p] = r.w[p];
+      }
     }
   }
 
   const int strips = (a.F + kUpCols - 1) / kUpCols, per_unit = (a.D + 63) / 64;
-  const int64_t total = (int64_t)*ch.n * strips * per_unit;
-  const int n = (int)min((int64_t)gridDim.x, total);
+  const int64_t units = (int64_t)*ch.n * strips, total = units * per_unit;
+  const int n = takers(units, per_unit, gridDim.x);
   if ((int)blockIdx.x >= n) return;
   const int64_t begin = share(total, blockIdx.x, n), end = share(total, blockIdx.x + 1, n);
   int64_t unit = begin / per_unit;
@@ -581,6 +627,7 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
           if (++strip == strips) strip = 0, ++x;
         }
       }
+    if (lane == 0 && warp == kWarps) ask_ahead(tm_d, a, ch);
     return;
   }
   // a warp has sixteen gate columns and the up columns that go with them, as two tiles of eight and eight
@@ -661,7 +708,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   const int strips = (a.D + kDownCols - 1) / kDownCols, per_expert = (a.F + 63) / 64, per_unit = chosen * per_expert;
   const int tiles = (a.M + 7) / 8;
   const int64_t total = (int64_t)strips * per_unit;
-  const int n = (int)min((int64_t)gridDim.x, total);
+  const int n = takers(strips, per_unit, gridDim.x);
   auto put = [&](int m, int c, float v) {
     if (a.y_f32) ((float *)a.Y)[(int64_t)m * a.ldy + c] = v;
     else ((__nv_bfloat16 *)a.Y)[(int64_t)m * a.ldy + c] = __float2bfloat16_rn(v);
@@ -789,7 +836,7 @@ MoeLayout moe_layout(const alg_moe_s &h, int64_t M) {
   return L;
 }
 
-using UpKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const MoeArgs);
+using UpKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const MoeArgs);
 using DownKernel = void (*)(const CUtensorMap, const CUtensorMap, const MoeArgs);
 UpKernel up_kernel(int tiles) {
   return tiles <= 1 ? moe_up_kernel<1> : tiles <= 2 ? moe_up_kernel<2> : tiles <= 4 ? moe_up_kernel<4> : moe_up_kernel<8>;
@@ -972,9 +1019,10 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
     if (make_map_nd(&tm_r, W_router, 2, dr, sr, br, 128) != cudaSuccess) return ALG_ERR_CUDA;
   }
   a.blocks = F % 64 == 0;
-  if (!fit_ring(a, true, kChunk + tiles * 1024, (size_t)M * kLogitCols * 4, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
+  a.down_ctas = h->num_sms, a.down_blocks = D % 64 == 0;
+  if (!fit_ring(a, true, kChunk + tiles * 1024, choose_bytes(a.M, a.E, a.k), &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
   a.count = h->d_state + 4;
-  if (launch_moe(up_kernel(tiles), h->clusters * kCluster, kCluster, smem, st, tm_up, tm_x, tm_r, a) != cudaSuccess) return ALG_ERR_CUDA;
+  if (launch_moe(up_kernel(tiles), h->clusters * kCluster, kCluster, smem, st, tm_up, tm_x, tm_r, tm_down, a) != cudaSuccess) return ALG_ERR_CUDA;
   a.blocks = D % 64 == 0;
   if (!fit_ring(a, false, kChunk + a.planes * tiles * 1024, 0, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
   a.count = h->d_state + 4 + h->num_sms;
