@@ -8,11 +8,13 @@
 // tells its peers.  Every cluster does that for itself (the router is read from L2), so no CTA waits for another cluster, and every CTA
 // knows the choice without a launch of its own for it.  An fp32 router is taken as three bf16 terms, which hold all its bits.
 //
-// Products.  A unit is 128 gate and the matching 128 up columns of one expert's bank or, for the down product, 256
-// columns of Y over all chosen experts; its reduction is cut into chunks of 64 weight rows (32 KB).  The chunks of all units in a row
+// Products.  A unit is 128 gate and the matching 128 up columns of one expert's bank, reduced over D in chunks of 64 weight rows or, for
+// the down product, 128 columns of Y over all chosen experts in chunks of 128 (32 KB either way).  The chunks of all units in a row
 // are dealt to the CTAs in equal consecutive shares, whatever the number of experts and rows.  A unit that lies in one CTA is finished
 // there.  The others leave their partial sums in the workspace, and whichever CTA counts itself the last of a unit adds them in CTA
-// order (so the sums are the same every time) and finishes it: nobody waits.
+// order (so the sums are the same every time) and finishes it: nobody waits.  Down sums are kept in shared memory by row of Y, so
+// that a product's steps of eight rows are full of the rows that take the expert at hand (40 rows, 128 experts: 2.7 rows, one step instead of
+// the 2.1 that hold them) and the parts that meet are no larger than Y.
 //
 // Weights come by tiled copies (boxes of 64 columns, 128-byte swizzle) through a ring of stages.  What limits such a stream is the
 // thread that asks for it, about 150 cycles a copy: with 16 KB in two copies 5.5 TB/s, 32 KB in one copy 6.6 to 7.1 (gate and up
@@ -22,6 +24,7 @@
 #include <cfloat>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "common.cuh"
 #include "rows.cuh"
@@ -50,8 +53,9 @@ constexpr int kWarps = 8, kConsumers = kWarps * 32, kThreads = kConsumers + 64; 
 constexpr int kCluster = 8;
 constexpr int kStages = 6;                  // at most
 constexpr int kBox = 64 * 64 * 2;           // 64 columns of 64 rows of weights
-constexpr int kChunk = 4 * kBox;            // up: [column block][gate, up]; down: [column block]
-constexpr int kUpCols = 128, kDownCols = 256;
+constexpr int kChunk = 4 * kBox;            // up: [column block][gate, up][64 rows]; down: [column block][128 rows]
+constexpr int kCols = 128;                  // of a unit (up: of the hidden state)
+constexpr int kUpPitch = 2 * kCols + 4, kDownPitch = kCols + 4;   // floats of a row of sums in shared memory
 constexpr int kAhead = 12;                  // chunks of a share of the second launch that the first asks into L2
 constexpr int kSmemLimit = 225 * 1024;
 constexpr int kMaxM = ALG_MOE_MAX_M;
@@ -72,14 +76,14 @@ struct MoeArgs {
   int *table;                 // workspace: the chosen experts, as `Chosen` lies in shared memory
   __nv_bfloat16 *H;           // workspace: weighted hidden rows, [planes][M * k][ldh]
   int ldh;                    // F to the next multiple of 64
-  float4 *part;               // workspace: partial sums, [CTA][2][8 warps][2][row tiles][32 lanes]
+  float4 *part;               // workspace: partial sums, [CTA][2][M][256] of the first launch, [..][128] of the second
   int down_ctas, down_blocks; // of the second launch
   int blocks;                 // tensor maps of whole column blocks (one copy a chunk)
   int *count;                 // [CTA]: arrivals at the unit whose first contributor it is
   int *status;
   long long wait_limit;
   int stages, stage_bytes;
-  int off_ring;               // the ring; in front of it what `Routes` points to
+  int off_sums, off_ring;     // sums by row; the ring; in front of them what `Chosen` and `Routes` point to
 };
 
 // The chosen experts in ascending order: what both launches go by.
@@ -372,7 +376,7 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&w)[4], uint3
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(b0), "r"(b1));
 }
-// Weights of a chunk, 16 columns of the warp by 64 rows: lanes 0-15 address rows 0-7 of the first and of the second eight
+// Weights, 16 columns of the warp by 64 rows: lanes 0-15 address rows 0-7 of the first and of the second eight
 // columns, lanes 16-31 rows 8-15; `box` and `byte_col` are those of the lane's eight.
 __device__ __forceinline__ void load_weights(uint32_t box, int byte_col, uint32_t (&w)[4][4]) {
   const int lane = threadIdx.x & 31, row = (lane & 7) + (lane >> 4 << 3);
@@ -415,50 +419,45 @@ __device__ __forceinline__ int takers(int64_t units, int per_unit, int ctas) {
 __device__ __forceinline__ int64_t share(int64_t total, int c, int n) { return total * c / n; }
 __device__ __forceinline__ int owner(int64_t total, int64_t chunk, int n) { return (int)(((chunk + 1) * n - 1) / total); }
 
-// The sums of a unit that several CTAs have parts of: leaves this CTA's and, in the last to come, adds all of them in CTA order.
-// True in that CTA.  All consumers.
-template <int NT>
-__device__ bool meet_parts(const MoeArgs &a, float (&acc)[2][NT][4], int nt, int64_t total, int n, int per_unit, int64_t unit, int *flag) {
-  const int me = blockIdx.x, tiles = (a.M + 7) / 8;
-  const int c0 = owner(total, unit * per_unit, n), c1 = owner(total, (unit + 1) * per_unit - 1, n);
-  if (c0 == c1) return true;
-  const size_t slot = (size_t)kWarps * 2 * tiles * 32;
-  // a CTA has at most two units it shares: the first of its share, and the last, where that is another one; all but the first
-  // contributor begin inside the unit
-  const int late = share(total, c0, n) / per_unit == unit ? 0 : 1;
-  float4 *const parts = a.part + (size_t)(threadIdx.x >> 5) * 2 * tiles * 32 + (threadIdx.x & 31);
-  float4 *const mine = parts + ((size_t)me * 2 + (me == c0 ? late : 0)) * slot;
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-      if (t < nt) __stcg(mine + (j * tiles + t) * 32, make_float4(acc[j][t][0], acc[j][t][1], acc[j][t][2], acc[j][t][3]));
-  consumer_barrier();
-  if (threadIdx.x == 0) {   // (what the barrier orders before its fence, the fence orders before its count)
-    __threadfence();
-    const bool last = atomicAdd(a.count + c0, 1) == c1 - c0;
-    if (last) a.count[c0] = 0;   // as the next launch finds it
-    __threadfence();
-    *flag = last;
+// Where the parts of a unit lie that CTAs c0 .. c1 have parts of.  A CTA has at most two units it shares: the first of its share, and the
+// last, where that is another one; all but the first contributor begin inside the unit.
+struct Parts {
+  int c0, c1;
+  int late;         // the first contributor's is its second
+  size_t slot;      // float4s of a part
+  float4 *part;
+  __device__ __forceinline__ Parts(const MoeArgs &a, int64_t total, int n, int per_unit, int64_t unit, int row_floats) {
+    c0 = owner(total, unit * per_unit, n), c1 = owner(total, (unit + 1) * per_unit - 1, n);
+    late = share(total, c0, n) / per_unit == unit ? 0 : 1;
+    slot = (size_t)a.M * row_floats / 4;
+    part = a.part;
   }
-  consumer_barrier();
-  if (!*flag) return false;   // (nobody writes it again before the barrier of another unit)
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-      if (t < nt) {
-        const float4 *p = parts + (j * tiles + t) * 32;
-        float4 sum = __ldcg(p + ((size_t)c0 * 2 + late) * slot);
-#pragma unroll 8
-        for (int c = c0 + 1; c <= c1; ++c) {
-          const float4 v = __ldcg(p + (size_t)c * 2 * slot);
-          sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-        }
-        acc[j][t][0] = sum.x, acc[j][t][1] = sum.y, acc[j][t][2] = sum.z, acc[j][t][3] = sum.w;
-      }
-  return true;
-}
+  __device__ __forceinline__ bool whole() const { return c0 == c1; }
+  __device__ __forceinline__ float4 *of(int c) const { return part + ((size_t)c * 2 + (c == c0 ? late : 0)) * slot; }
+  __device__ __forceinline__ float4 sum(int at) const {   // in CTA order
+    float4 s = __ldcg(of(c0) + at);
+    const float4 *p = part + at;
+#pragma unroll 4
+    for (int c = c0 + 1; c <= c1; ++c) {
+      const float4 v = __ldcg(p + (size_t)c * 2 * slot);
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    return s;
+  }
+  // After this CTA's part: is it the last?  All consumers.
+  __device__ __forceinline__ bool last(const MoeArgs &a, int *flag) const {
+    consumer_barrier();
+    if (threadIdx.x == 0) {   // (what the barrier orders before its fence, the fence orders before its count)
+      __threadfence();
+      const bool l = atomicAdd(a.count + c0, 1) == c1 - c0;
+      if (l) a.count[c0] = 0;   // as the next launch finds it
+      __threadfence();
+      *flag = l;
+    }
+    consumer_barrier();
+    return *flag;   // (nobody writes it again before the barrier of another unit)
+  }
+};
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
   asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst), "l"(map),
@@ -470,16 +469,16 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map
 
 // The first chunks of every share of the second launch are asked into L2, so that HBM does not idle between the launches.
 __device__ void ask_ahead(const CUtensorMap &tm_d, const MoeArgs &a, const Chosen &ch) {
-  const int per_expert = (a.F + 63) / 64, chosen = *ch.n, per_unit = chosen * per_expert;
-  const int strips = (a.D + kDownCols - 1) / kDownCols, n = takers(strips, per_unit, a.down_ctas);
+  const int per_expert = (a.F + 127) / 128, chosen = *ch.n, per_unit = chosen * per_expert;
+  const int strips = (a.D + kCols - 1) / kCols, n = takers(strips, per_unit, a.down_ctas);
   const int64_t total = (int64_t)strips * per_unit;
   for (int c = blockIdx.x; c < n; c += gridDim.x) {
     const int64_t begin = share(total, c, n), end = min(share(total, c + 1, n), begin + kAhead);
     for (int64_t i = begin; i < end; ++i) {
       const int unit = (int)(i / per_unit), at = (int)(i - (int64_t)unit * per_unit), x = at / per_expert;
       if (a.down_blocks)
-        asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(&tm_d), "r"(0), "r"((at - x * per_expert) * 64),
-                     "r"(unit * 4), "r"(ch.expert[x]));
+        asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(&tm_d), "r"(0), "r"((at - x * per_expert) * 128),
+                     "r"(unit * 2), "r"(ch.expert[x]));
     }
   }
 }
@@ -595,7 +594,7 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
     }
   }
 
-  const int strips = (a.F + kUpCols - 1) / kUpCols, per_unit = (a.D + 63) / 64;
+  const int strips = (a.F + kCols - 1) / kCols, per_unit = (a.D + 63) / 64;
   const int64_t units = (int64_t)*ch.n * strips, total = units * per_unit;
   const int n = takers(units, per_unit, gridDim.x);
   if ((int)blockIdx.x >= n) return;
@@ -617,8 +616,8 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
           if (a.blocks) {
             tma_load_5d(st, &tm_w, bar, 0, chunk * 64, 0, strip * 2, e);
           } else {
-            tma_load_4d(st, &tm_w, bar, strip * kUpCols, chunk * 64, 0, e);
-            tma_load_4d(st + 2 * kBox, &tm_w, bar, strip * kUpCols + 64, chunk * 64, 0, e);
+            tma_load_4d(st, &tm_w, bar, strip * kCols, chunk * 64, 0, e);
+            tma_load_4d(st + 2 * kBox, &tm_w, bar, strip * kCols + 64, chunk * 64, 0, e);
           }
         }
         ring.next();
@@ -632,53 +631,84 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
   }
   // a warp has sixteen gate columns and the up columns that go with them, as two tiles of eight and eight
   const int box = (warp >> 2) * 2 * kBox + ((lane >> 3) & 1) * kBox, byte_col = (warp & 3) * 32;
+  float *sums = (float *)(smem + a.off_sums);   // eight rows of 128 gate and 128 up sums
   for (int64_t i = begin; i < end; ++unit) {
     const uint2 mask = ch.mask[x];
-    const int rows = rows_of(mask), nt = (rows + 7) / 8;
-    float acc[2][NT][4];
-    int x_row[NT];   // the row of X this lane addresses in each tile
+    const int rows = rows_of(mask), first = ch.first[x];
+    const Parts parts(a, total, n, per_unit, unit, 2 * kCols);
+    // four hidden values of a pair, from their gate and up sums
+    auto finish = [&](int row, int c, float4 gate, float4 up) {
+      const int col = strip * kCols + c;
+      if (col >= a.ldh) return;   // (columns from F on come out as zero: their weights are)
+      const float w = r.pair_w[first + row];
+      auto hidden = [&](float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u * w; };
+      float v[4] = {hidden(gate.x, up.x), hidden(gate.y, up.y), hidden(gate.z, up.z), hidden(gate.w, up.w)};
+      __nv_bfloat16 *dst = a.H + (size_t)(first + row) * a.ldh + col;
+      for (int p = 0; p < a.planes; ++p) {
+        __nv_bfloat16 b[4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[0][t][e] = acc[1][t][e] = 0.f;
-      x_row[t] = t < nt ? nth_row(mask, min(t * 8 + (lane & 7), rows - 1)) : 0;
-    }
-    for (; chunk < per_unit && i < end; ++chunk, ++i) {
-      ring.wait_full(a);
-      const uint32_t st = ring.stage(), xs = st + kChunk;
-      uint32_t w[2][4][4];
-      load_weights(st + box, byte_col, w[0]);
-      load_weights(st + box, byte_col + 16, w[1]);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if (t >= nt) continue;
-        product(w, xs + x_row[t] * 128, (x_row[t] & 7) << 4, acc, t);
+        for (int e = 0; e < 4; ++e) {
+          b[e] = __float2bfloat16_rn(v[e]);
+          const float back = __bfloat162float(b[e]);
+          v[e] = isfinite(back) ? v[e] - back : 0.f;
+        }
+        *(uint2 *)(dst + (size_t)p * P * a.ldh) = *(const uint2 *)b;
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
-      ring.next();
-    }
-    if (meet_parts<NT>(a, acc, nt, total, n, per_unit, unit, &flag)) {
+    };
+    auto body = [&](auto tiles_of) {
+      constexpr int N = decltype(tiles_of)::value;
+      float acc[2][N][4];
+      int x_row[N];   // the row of X this lane addresses in each tile
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int t = 0; t < N; ++t) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int e = 0; e < 4; ++e) acc[0][t][e] = acc[1][t][e] = 0.f;
+        x_row[t] = nth_row(mask, min(t * 8 + (lane & 7), rows - 1));
+      }
+      for (; chunk < per_unit && i < end; ++chunk, ++i) {
+        ring.wait_full(a);
+        const uint32_t st = ring.stage(), xs = st + kChunk;
+        uint32_t w[2][4][4];
+        load_weights(st + box, byte_col, w[0]);
+        load_weights(st + box, byte_col + 16, w[1]);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int row = t * 8 + (lane & 3) * 2 + h, col = strip * kUpCols + warp * 16 + j * 8 + (lane >> 2);
-            if (row >= rows || col >= a.ldh) continue;   // (columns from F on come out as zero: their weights are)
-            const int pair = ch.first[x] + row;
-            const float gate = acc[j][t][h], up = acc[j][t][2 + h];
-            float v = __fdividef(gate, 1.f + __expf(-gate)) * up * r.pair_w[pair];
-            __nv_bfloat16 *dst = a.H + (size_t)pair * a.ldh + col;
-            for (int p = 0; p < a.planes; ++p) {
-              const __nv_bfloat16 b = __float2bfloat16_rn(v);
-              dst[(size_t)p * P * a.ldh] = b;
-              const float back = __bfloat162float(b);
-              v = isfinite(back) ? v - back : 0.f;
-            }
-          }
-    }
+        for (int t = 0; t < N; ++t)
+          if (t * 8 < rows) product(w, xs + x_row[t] * 128, (x_row[t] & 7) << 4, acc, t);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
+        ring.next();
+      }
+      // eight rows at a time, four columns a thread
+#pragma unroll
+      for (int t = 0; t < N; ++t) {
+        if (t * 8 >= rows) continue;
+        consumer_barrier();
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sums[((lane & 3) * 2 + (e & 1)) * kUpPitch + (e >> 1) * kCols + warp * 16 + j * 8 + (lane >> 2)] = acc[j][t][e];
+        consumer_barrier();
+        const int row = t * 8 + (tid >> 5), c = (tid & 31) * 4;
+        if (row >= rows) continue;
+        const float4 gate = *(const float4 *)(sums + (tid >> 5) * kUpPitch + c), up = *(const float4 *)(sums + (tid >> 5) * kUpPitch + kCols + c);
+        if (parts.whole()) {
+          finish(row, c, gate, up);
+        } else {
+          float4 *mine = parts.of(blockIdx.x) + row * (2 * kCols / 4) + c / 4;
+          __stcg(mine, gate), __stcg(mine + kCols / 4, up);
+        }
+      }
+    };
+    if (NT == 1 || rows <= 8) body(std::integral_constant<int, 1>());
+    else if (NT == 2 || rows <= 16) body(std::integral_constant<int, NT < 2 ? NT : 2>());
+    else if (NT == 4 || rows <= 32) body(std::integral_constant<int, NT < 4 ? NT : 4>());
+    else body(std::integral_constant<int, NT>());
+    if (!parts.whole() && parts.last(a, &flag))
+      for (int e = tid; e < rows * (kCols / 4); e += kConsumers) {
+        const int row = e >> 5, c = e & 31;
+        finish(row, c * 4, parts.sum(row * (2 * kCols / 4) + c), parts.sum(row * (2 * kCols / 4) + kCols / 4 + c));
+      }
     chunk = 0;
     if (++strip == strips) strip = 0, ++x;
   }
@@ -705,16 +735,20 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   for (int i = tid; i < Chosen::words(most, a.M); i += kThreads) ((int *)smem)[i] = a.table[i];
   __syncthreads();
   const int chosen = *ch.n;
-  const int strips = (a.D + kDownCols - 1) / kDownCols, per_expert = (a.F + 63) / 64, per_unit = chosen * per_expert;
-  const int tiles = (a.M + 7) / 8;
+  const int strips = (a.D + kCols - 1) / kCols, per_expert = (a.F + 127) / 128, per_unit = chosen * per_expert;
   const int64_t total = (int64_t)strips * per_unit;
   const int n = takers(strips, per_unit, gridDim.x);
-  auto put = [&](int m, int c, float v) {
-    if (a.y_f32) ((float *)a.Y)[(int64_t)m * a.ldy + c] = v;
-    else ((__nv_bfloat16 *)a.Y)[(int64_t)m * a.ldy + c] = __float2bfloat16_rn(v);
+  // eight columns' sums of a row of Y (D is a multiple of eight)
+  auto put = [&](int m, int c, const float4 &u, const float4 &v) {
+    if (c >= a.D) return;
+    const float rest = ch.rest[m];
+    const float f[8] = {u.x + rest, u.y + rest, u.z + rest, u.w + rest, v.x + rest, v.y + rest, v.z + rest, v.w + rest};
+    if (a.y_f32) store8((float *)a.Y + (int64_t)m * a.ldy + c, f);
+    else store8((__nv_bfloat16 *)a.Y + (int64_t)m * a.ldy + c, f);
   };
   if (total == 0) {   // nobody takes an expert
-    for (int i = blockIdx.x * kThreads + tid; i < a.M * a.D; i += gridDim.x * kThreads) put(i / a.D, i % a.D, ch.rest[i / a.D]);
+    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = blockIdx.x * kThreads + tid; i < a.M * (a.D / 8); i += gridDim.x * kThreads) put(i / (a.D / 8), i % (a.D / 8) * 8, none, none);
     return;
   }
   if ((int)blockIdx.x >= n) return;
@@ -723,7 +757,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   int64_t unit = begin / per_unit;
   const int at = (int)(begin - unit * per_unit);
   int x = at / per_expert, chunk = at - x * per_expert;
-  const int group_bytes = a.planes * 1024;   // eight hidden rows
+  const int group_bytes = a.planes * 2048;   // eight hidden rows: [plane][64 columns, 64 more][8]
   if (warp >= kWarps) {
     if (lane == 0)
       for (int64_t i = begin; i < end; ++i) {
@@ -732,14 +766,15 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         if (warp > kWarps) {
           const int p0 = ch.first[x], groups = (ch.first[x + 1] - p0 + 7) / 8;
           mbar_expect_tx(bar, groups * group_bytes);
-          for (int g = 0; g < groups; ++g) tma_load_3d(st + kChunk + g * group_bytes, &tm_h, bar, chunk * 64, p0 + g * 8, 0);
+          for (int g = 0; g < groups; ++g) tma_load_4d(st + kChunk + g * group_bytes, &tm_h, bar, 0, p0 + g * 8, chunk * 2, 0);
         } else {
           mbar_expect_tx(bar, kChunk);
           const int e = ch.expert[x];
           if (a.blocks) {
-            tma_load_4d(st, &tm_w, bar, 0, chunk * 64, (int)unit * 4, e);
+            tma_load_4d(st, &tm_w, bar, 0, chunk * 128, (int)unit * 2, e);
           } else {
-            for (int b = 0; b < 4; ++b) tma_load_3d(st + b * kBox, &tm_w, bar, (int)unit * kDownCols + b * 64, chunk * 64, e);
+            tma_load_3d(st, &tm_w, bar, (int)unit * kCols, chunk * 128, e);
+            tma_load_3d(st + 2 * kBox, &tm_w, bar, (int)unit * kCols + 64, chunk * 128, e);
           }
         }
         ring.next();
@@ -750,69 +785,89 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       }
     return;
   }
-  // a warp has 32 columns, as two tiles of sixteen
-  const int box = (warp >> 1) * kBox, byte_col = (warp & 1) * 64 + ((lane >> 3) & 1) * 16;
+  // a warp has sixteen columns
+  const int box = (warp >> 2) * 2 * kBox, byte_col = (warp & 3) * 32 + ((lane >> 3) & 1) * 16;
+  float *sums = (float *)(smem + a.off_sums);   // [M][128]; a warp adds to its own columns
   for (int64_t i = begin; i < end; ++unit) {
-    float acc[2][NT][4];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[0][t][e] = acc[1][t][e] = 0.f;
+    for (int e = tid; e < a.M * kDownPitch; e += kConsumers) sums[e] = 0.f;
+    consumer_barrier();
     for (; x < chosen && i < end; ++x, chunk = 0) {
       const uint2 mask = ch.mask[x];
-      for (; chunk < per_expert && i < end; ++chunk, ++i) {
-        ring.wait_full(a);
-        const uint32_t st = ring.stage(), hs = st + kChunk;
-        uint32_t w[2][4][4];
-        load_weights(st + box, byte_col, w[0]);
-        load_weights(st + box, byte_col + 32, w[1]);
+      const int rows = rows_of(mask);
+      auto body = [&](auto tiles_of) {
+        constexpr int N = decltype(tiles_of)::value;
+        float acc[N][4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const uint32_t here = (t < 4 ? mask.x : mask.y) >> (8 * (t & 3)) & 255u;   // rows of the tile that take the expert
-          if (!here) continue;
-          const int m = t * 8 + (lane & 7), row = takes(mask, m) ? rows_below(mask, m) : 0;
-          const uint32_t h = hs + (row >> 3) * group_bytes + (row & 7) * 128;
-          const int sw = (row & 7) << 4;
-          float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-          for (int p = 0; p < a.planes; ++p) {
-            uint32_t b[4], c[4];
-            ldmatrix4(h + p * 1024 + (((lane >> 3) * 16) ^ sw), b);
-            ldmatrix4(h + p * 1024 + ((64 + (lane >> 3) * 16) ^ sw), c);
+        for (int t = 0; t < N; ++t)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) mma(d[j], w[j][0], b[0], b[1]);
+          for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
+        for (; chunk < per_expert && i < end; ++chunk, ++i) {
+          ring.wait_full(a);
+          const uint32_t st = ring.stage(), hs = st + kChunk + (lane & 7) * 128;
+          const int sw = (lane & 7) << 4;
+          uint32_t w[2][4][4];
+          load_weights(st + box, byte_col, w[0]);
+          load_weights(st + box + kBox, byte_col, w[1]);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) mma(d[j], w[j][1], b[2], b[3]);
+          for (int t = 0; t < N; ++t) {
+            if (t * 8 >= rows) continue;
+            float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            for (int p = 0; p < a.planes; ++p) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) mma(d[j], w[j][2], c[0], c[1]);
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t at = hs + t * group_bytes + p * 2048 + h * 1024;
+                uint32_t b[4], c[4];
+                ldmatrix4(at + (((lane >> 3) * 16) ^ sw), b);
+                ldmatrix4(at + ((64 + (lane >> 3) * 16) ^ sw), c);
+                mma(d[h], w[h][0], b[0], b[1]);
+                mma(d[h], w[h][1], b[2], b[3]);
+                mma(d[h], w[h][2], c[0], c[1]);
+                mma(d[h], w[h][3], c[2], c[3]);
+              }
+            }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) mma(d[j], w[j][3], c[2], c[3]);
+            for (int e = 0; e < 4; ++e) acc[t][e] += d[0][e] + d[1][e];
           }
-          // (the other rows' columns hold whatever the stage did)
-          const bool k0 = here >> (2 * (lane & 3)) & 1u, k1 = here >> (2 * (lane & 3) + 1) & 1u;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            if (k0) acc[j][t][0] += d[j][0], acc[j][t][2] += d[j][2];
-            if (k1) acc[j][t][1] += d[j][1], acc[j][t][3] += d[j][3];
-          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
+          ring.next();
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
-        ring.next();
-      }
+        // to the rows that take the expert
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int row = t * 8 + (lane & 3) * 2 + h;
+            if (row >= rows) continue;
+            float *to = sums + nth_row(mask, row) * kDownPitch + warp * 16 + (lane >> 2);
+            to[0] += acc[t][h], to[8] += acc[t][2 + h];
+          }
+      };
+      if (NT == 1 || rows <= 8) body(std::integral_constant<int, 1>());
+      else if (NT == 2 || rows <= 16) body(std::integral_constant<int, NT < 2 ? NT : 2>());
+      else if (NT == 4 || rows <= 32) body(std::integral_constant<int, NT < 4 ? NT : 4>());
+      else body(std::integral_constant<int, NT>());
       if (chunk < per_expert) break;   // the share ends inside the expert
     }
     x = 0, chunk = 0;
-    if (meet_parts<NT>(a, acc, tiles, total, n, per_unit, unit, &flag)) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int m = t * 8 + (lane & 3) * 2 + (e & 1), c = (int)unit * kDownCols + warp * 32 + j * 16 + (lane >> 2) + (e >> 1) * 8;
-            if (m < a.M && c < a.D) put(m, c, acc[j][t][e] + ch.rest[m]);
-          }
+    consumer_barrier();
+    const Parts parts(a, total, n, per_unit, unit, kCols);
+    for (int e = tid; e < a.M * (kCols / 8); e += kConsumers) {
+      const int m = e / (kCols / 8), c = e % (kCols / 8);
+      const float4 u = *(const float4 *)(sums + m * kDownPitch + c * 8), v = *(const float4 *)(sums + m * kDownPitch + c * 8 + 4);
+      if (parts.whole()) {
+        put(m, (int)unit * kCols + c * 8, u, v);
+      } else {
+        float4 *mine = parts.of(blockIdx.x) + m * (kCols / 4) + c * 2;
+        __stcg(mine, u), __stcg(mine + 1, v);
+      }
     }
+    if (!parts.whole() && parts.last(a, &flag))
+      for (int e = tid; e < a.M * (kCols / 8); e += kConsumers) {
+        const int m = e / (kCols / 8), c = e % (kCols / 8), at = m * (kCols / 4) + c * 2;
+        put(m, (int)unit * kCols + c * 8, parts.sum(at), parts.sum(at + 1));
+      }
+    consumer_barrier();
   }
 }
 
@@ -831,7 +886,7 @@ MoeLayout moe_layout(const alg_moe_s &h, int64_t M) {
   size_t off = 0;
   L.table = off, off = up256(off + (size_t)Chosen::words(most_chosen((int)P, h.E), (int)M) * 4);
   L.h = off, off = up256(off + 3 * P * hidden_pitch(h.F) * 2);
-  L.part = off, off = up256(off + (size_t)h.num_sms * 2 * kWarps * 2 * row_tiles(M) * 512);
+  L.part = off, off = up256(off + (size_t)h.num_sms * 2 * M * 2 * kCols * sizeof(float));
   L.total = off;
   return L;
 }
@@ -856,9 +911,10 @@ cudaError_t moe_attributes() {
   });
 }
 // Ring behind the tables: as many stages as fit.
-bool fit_ring(MoeArgs &a, bool routes, int stage_bytes, size_t scratch, size_t *smem) {
+bool fit_ring(MoeArgs &a, bool routes, size_t sums, int stage_bytes, size_t scratch, size_t *smem) {
   const int P = a.M * a.k, table = (Chosen::words(most_chosen(P, a.E), a.M) * 4 + 7) / 8 * 8;
-  a.off_ring = (int)((table + (routes ? Routes::bytes(P, a.E) : 0) + 1023) / 1024 * 1024);
+  a.off_sums = (int)((table + (routes ? Routes::bytes(P, a.E) : 0) + 15) / 16 * 16);
+  a.off_ring = (int)((a.off_sums + sums + 1023) / 1024 * 1024);
   a.stage_bytes = stage_bytes;
   a.stages = (kSmemLimit - 1024 - a.off_ring) / stage_bytes;
   if (a.stages > kStages) a.stages = kStages;
@@ -997,19 +1053,19 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   if (e != cudaSuccess) return ALG_ERR_CUDA;
   if (D % 64 == 0) {   // {column of a block, row, column block, expert}
     const uint64_t d[4] = {64, F, D / 64, E}, s[3] = {down_row, 128, down_row * F};
-    const uint32_t b[4] = {64, 64, 4, 1};
+    const uint32_t b[4] = {64, 128, 2, 1};
     e = make_map_nd(&tm_down, W_down, 4, d, s, b, 128);
   } else {
     const uint64_t d[3] = {D, F, E}, s[2] = {down_row, down_row * F};
-    const uint32_t b[3] = {64, 64, 1};
+    const uint32_t b[3] = {64, 128, 1};
     e = make_map_nd(&tm_down, W_down, 3, d, s, b, 128);
   }
   if (e != cudaSuccess) return ALG_ERR_CUDA;
   const uint64_t dx[2] = {D, (uint64_t)M}, sx[1] = {(uint64_t)ldx * 2};
   const uint32_t bx[2] = {64, (uint32_t)M};
-  const uint64_t dh[3] = {H, (uint64_t)P, 3}, sh[2] = {2 * H, 2 * P * H};
-  const uint32_t bh[3] = {64, 8, (uint32_t)a.planes};
-  if (make_map_nd(&tm_x, X, 2, dx, sx, bx, 128) != cudaSuccess || make_map_nd(&tm_h, a.H, 3, dh, sh, bh, 128) != cudaSuccess) return ALG_ERR_CUDA;
+  const uint64_t dh[4] = {64, (uint64_t)P, H / 64, 3}, sh[3] = {2 * H, 128, 2 * P * H};   // {column of a block, pair, column block, plane}
+  const uint32_t bh[4] = {64, 8, 2, (uint32_t)a.planes};
+  if (make_map_nd(&tm_x, X, 2, dx, sx, bx, 128) != cudaSuccess || make_map_nd(&tm_h, a.H, 4, dh, sh, bh, 128) != cudaSuccess) return ALG_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   size_t smem = 0;
   CUtensorMap tm_r = tm_x;
@@ -1020,11 +1076,11 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   }
   a.blocks = F % 64 == 0;
   a.down_ctas = h->num_sms, a.down_blocks = D % 64 == 0;
-  if (!fit_ring(a, true, kChunk + tiles * 1024, choose_bytes(a.M, a.E, a.k), &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
+  if (!fit_ring(a, true, 8 * kUpPitch * sizeof(float), kChunk + tiles * 1024, choose_bytes(a.M, a.E, a.k), &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
   a.count = h->d_state + 4;
   if (launch_moe(up_kernel(tiles), h->clusters * kCluster, kCluster, smem, st, tm_up, tm_x, tm_r, tm_down, a) != cudaSuccess) return ALG_ERR_CUDA;
   a.blocks = D % 64 == 0;
-  if (!fit_ring(a, false, kChunk + a.planes * tiles * 1024, 0, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
+  if (!fit_ring(a, false, (size_t)a.M * kDownPitch * sizeof(float), kChunk + a.planes * tiles * 2048, 0, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
   a.count = h->d_state + 4 + h->num_sms;
   return launch_moe(down_kernel(tiles), h->num_sms, 1, smem, st, tm_down, tm_h, a) == cudaSuccess ? ALG_OK : ALG_ERR_CUDA;
 }
