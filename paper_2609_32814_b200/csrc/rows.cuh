@@ -22,6 +22,11 @@ template <>
 struct Raw8<__nv_bfloat16> {
   uint4 a;
   __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = *(const uint4 *)p; }
+  __device__ __forceinline__ void load4(int half, const __nv_bfloat16 *p) {   // four of them
+    const uint2 v = *(const uint2 *)p;
+    if (half) a.z = v.x, a.w = v.y;
+    else a.x = v.x, a.y = v.y;
+  }
   __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void set(int j, __nv_bfloat16 v) { ((__nv_bfloat16 *)&a)[j] = v; }
   __device__ __forceinline__ void get(float (&f)[8]) const {
@@ -34,6 +39,7 @@ template <>
 struct Raw8<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
+  __device__ __forceinline__ void load4(int half, const float *p) { (half ? b : a) = *(const float4 *)p; }
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ void set(int j, float v) { (j < 4 ? (float *)&a : (float *)&b)[j & 3] = v; }
   __device__ __forceinline__ void get(float (&f)[8]) const {
@@ -49,9 +55,80 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&f)[8]) {
   }
   *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float a, float b, float c, float d) {
+  const __nv_bfloat162 u = __floats2bfloat162_rn(a, b), v = __floats2bfloat162_rn(c, d);
+  *(uint2 *)p = make_uint2(*(const uint32_t *)&u, *(const uint32_t *)&v);
+}
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *(float4 *)p = make_float4(a, b, c, d); }
 __device__ __forceinline__ void store8(float *p, const float (&f)[8]) {
   ((float4 *)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
   ((float4 *)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+
+// Eight values as four pairs, for the packed fp32 instructions: half as many issue slots as one value at a time.
+struct F8 {
+  uint64_t p[4];
+};
+// (moves between a pair and its halves, not shifts and ors: those cost instructions)
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void halves(uint64_t p, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ F8 all8(float v) {
+  const uint64_t p = pair(v, v);
+  return {{p, p, p, p}};
+}
+__device__ __forceinline__ F8 operator*(const F8 &a, const F8 &b) {
+  return {{pair_mul(a.p[0], b.p[0]), pair_mul(a.p[1], b.p[1]), pair_mul(a.p[2], b.p[2]), pair_mul(a.p[3], b.p[3])}};
+}
+__device__ __forceinline__ F8 operator+(const F8 &a, const F8 &b) {
+  return {{pair_add(a.p[0], b.p[0]), pair_add(a.p[1], b.p[1]), pair_add(a.p[2], b.p[2]), pair_add(a.p[3], b.p[3])}};
+}
+__device__ __forceinline__ F8 operator*(const F8 &a, float b) { return a * all8(b); }
+__device__ __forceinline__ F8 operator+(const F8 &a, float b) { return a + all8(b); }
+__device__ __forceinline__ F8 fma8(const F8 &a, const F8 &b, const F8 &c) {
+  return {{pair_fma(a.p[0], b.p[0], c.p[0]), pair_fma(a.p[1], b.p[1], c.p[1]), pair_fma(a.p[2], b.p[2], c.p[2]), pair_fma(a.p[3], b.p[3], c.p[3])}};
+}
+__device__ __forceinline__ F8 fma8(const F8 &a, float b, const F8 &c) { return fma8(a, all8(b), c); }
+__device__ __forceinline__ F8 from8(const float (&f)[8]) { return {{pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7])}}; }
+__device__ __forceinline__ void to8(const F8 &a, float (&f)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) halves(a.p[j], f[2 * j], f[2 * j + 1]);
+}
+__device__ __forceinline__ float sum8(const F8 &a) {
+  float lo, hi;
+  halves(pair_add(pair_add(a.p[0], a.p[1]), pair_add(a.p[2], a.p[3])), lo, hi);
+  return lo + hi;
+}
+// The sum of eight products.
+__device__ __forceinline__ float dot8(const F8 &a, const F8 &b) {
+  float lo, hi;
+  halves(pair_add(pair_fma(a.p[0], b.p[0], pair_mul(a.p[1], b.p[1])), pair_fma(a.p[2], b.p[2], pair_mul(a.p[3], b.p[3]))), lo, hi);
+  return lo + hi;
+}
+// 1 / (1 + exp(-x)), within 4 units: two approximations of the special function unit.
+__device__ __forceinline__ float sigmoid(float x) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
 }
 
 inline size_t elem_size(alg_dtype_t t) { return t == ALG_BF16 ? 2 : 4; }
