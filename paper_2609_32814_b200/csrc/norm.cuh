@@ -1,0 +1,617 @@
+// A block's border: Y = R + alpha * scale * g * (norm(F) * w + b) and N = norm(Y) * w' + b', and the gradients of both.
+//
+// A row is D <= 8192 features, read and written once: bound by HBM, if the arithmetic is kept short (72 instructions a value
+// took twice the time of the bytes).  A group of T threads takes a row at a time, eight columns a thread (16 past 4096); the rows of its
+// operands come into shared memory by the bulk copy engine, `stages` rows ahead, so that what is in flight does not depend on how
+// many registers the arithmetic takes.  Vectors are folded once a CTA (alpha * scale * post_weight, ...) and kept in shared memory; arithmetic is on
+// pairs; up to four sums cross the group in one exchange.
+// Gradient of v = (x - mean) r, r = 1 / sqrt(var + eps), for a gradient h of v:
+//     dx = r (h - mean(h) - v mean(h v))       (RMS: without mean(h), mean(x) = 0)
+// Column sums: with a = dR * g every vector behind F needs only P = sum_b a v and Q = sum_b a:
+//     d_post_weight = alpha scale P,  d_post_bias = alpha scale Q,  d_scale = alpha (post_weight P + post_bias Q).
+// A thread keeps the sums of its columns over all rows of its group in registers, the groups of a CTA meet in shared memory at the end, and
+// a second launch adds the CTAs' sums in CTA order.
+#pragma once
+
+#include "common.cuh"
+#include "rows.cuh"
+#include "tc_common.cuh"
+
+namespace algproj {
+
+struct NormArgs;
+// One translation unit for each direction and type of the residual stream (F, gate and N bf16): the kernels with their form as a constant.
+cudaError_t launch_norm_forward_bf16(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_forward_f32(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_bf16(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_f32(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
+
+
+constexpr int kMaxStages = 4;
+constexpr int kMaxGroups = 15;             // named barriers 1 .. 15
+constexpr int kBudget = 224 * 1024;        // shared memory of a CTA for its vectors and rows
+constexpr int kVectorBytes = 64 * 1024;    // folded vectors that are kept in shared memory
+constexpr int kNarrow = 4096;              // widest row of eight columns a thread
+constexpr int kThreads = 512;              // of a CTA, at most
+constexpr int kSums = 4;                   // column sums: dN * v, dN, P, Q
+
+enum { kX, kT, kN, kF, kG, kOps };          // operands: R or Y, dY, dN, F, gate of each element
+struct NormArgs {
+  uint32_t M;
+  int D, T, G, stages;
+  int flags, layer;
+  float eps, alpha;
+  const uint8_t *op[kOps];      // rows of the operands, nullptr for none
+  uint32_t pitch[kOps], bytes[kOps];   // bytes between rows, of a row
+  int at[kOps], stage_bytes;    // where a row lies in a stage
+  const void *gate;             // of each row
+  const float *post_w, *post_b, *scale, *pre_w, *pre_b;
+  uint8_t *y, *out;             // forward: Y, N; backward: dR, dF
+  uint8_t *dg;                  // backward: gradient of the gate
+  uint32_t pitch_y, pitch_out, pitch_dg;
+  int vectors;                  // bytes of the folded vectors in shared memory; 0: read where they lie
+  float *part;                  // [CTAs][kSums][D]
+  int *status;
+  long long wait_limit;
+};
+
+// The form of a call: what it does, as a constant of a kernel (kAny: found out at run time, with every branch that costs: gradients of
+// 16384 x 4096 rows 467 us against 320).
+enum { kFormPre = 1, kFormPost = 2, kFormJoin = 4, kFormGate = 8, kAny = -1 };   // + kFormGate * gate
+enum { kGateNone, kGateRow, kGateElement, kGateSigmoid };   // a row's gate asks for its sigmoid at run time
+
+namespace {
+
+// Shared memory of a CTA: barriers, the reductions' two slots, then the rows.
+constexpr int kBarBytes = kMaxGroups * kMaxStages * 8;
+constexpr int kRedBytes = 2 * 32 * 16;   // two slots of one float4 for each warp
+constexpr int kRowsAt = (kBarBytes + kRedBytes + 127) / 128 * 128;
+
+__device__ __forceinline__ void group_barrier(int g, int T) {
+  if (T == 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "r"(T) : "memory");
+}
+// Sums of up to four values over the group's threads, to all of them.  In a warp the lanes halve the values between them (six
+// exchanges for four values, not twenty), then each lane fetches one value of every eighth warp.  Two slots in turn: a thread that
+// writes a slot again has passed the barrier behind everybody's reading of it.
+template <int K>
+__device__ __forceinline__ void group_sum(float (&v)[K], float4 *red, int &turn, int g, int T) {
+  const int lane = threadIdx.x & 31;
+  float r;   // of value lane & 3 (K > 2), lane & 1 (K = 2), or the only one
+  if (K == 1) {
+    r = v[0];
+  } else {
+    float a0, a1;
+    if (K > 2) {
+      const float hi0 = v[K > 2 ? 2 : 0], hi1 = K > 3 ? v[K > 3 ? 3 : 0] : 0.f, lo0 = v[0], lo1 = v[K > 1 ? 1 : 0];
+      const bool up = lane & 2;
+      a0 = (up ? hi0 : lo0) + __shfl_xor_sync(~0u, up ? lo0 : hi0, 2);
+      a1 = (up ? hi1 : lo1) + __shfl_xor_sync(~0u, up ? lo1 : hi1, 2);
+    } else {
+      a0 = v[0], a1 = v[K > 1 ? 1 : 0];
+    }
+    const bool odd = lane & 1;
+    r = (odd ? a1 : a0) + __shfl_xor_sync(~0u, odd ? a0 : a1, 1);
+  }
+  if (K == 1) r += __shfl_xor_sync(~0u, r, 1);
+  if (K <= 2) r += __shfl_xor_sync(~0u, r, 2);
+  r += __shfl_xor_sync(~0u, r, 4);
+  r += __shfl_xor_sync(~0u, r, 8);
+  r += __shfl_xor_sync(~0u, r, 16);
+  constexpr int kValues = K > 2 ? 4 : K;
+  if (T > 32) {
+    const int warps = T >> 5, first = g * warps, mine = (threadIdx.x >> 5) - first;
+    float *slot = (float *)(red + turn * 32 + first);
+    turn ^= 1;
+    if (lane < kValues) slot[mine * kValues + lane] = r;
+    group_barrier(g, T);
+    r = 0.f;
+    for (int i = lane; i < warps * kValues; i += 32) r += slot[i];
+#pragma unroll
+    for (int o = kValues; o < 32; o <<= 1) r += __shfl_xor_sync(~0u, r, o);
+  } else {
+    __syncwarp();   // (a barrier of the group, as callers count on)
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = K == 1 ? r : __shfl_sync(~0u, r, k);
+}
+
+// A thread's pieces of eight columns.  Rows on 16 bytes: eight consecutive ones, or, where operands are fp32, four and four that lie
+// T * 4 columns apart (eight fp32 values in a row would have every second thread's 16 bytes meet in the same banks).  Else every T-th
+// column, whose scalar accesses coalesce.
+// kWhole: every thread's pieces are inside the row, nothing is asked.
+enum { kScalar, kEight, kFours, kWhole = 4 };
+template <int HOW>
+struct Cols {
+  static constexpr int MAP = HOW & 3;
+  int t, T, D;
+  __device__ __forceinline__ int at(int v, int j) const {
+    return MAP == kEight ? (v * T + t) * 8 + j : MAP == kFours ? ((2 * v + (j >> 2)) * T + t) * 4 + (j & 3) : t + (v * 8 + j) * T;
+  }
+  __device__ __forceinline__ bool on(int v, int j) const { return HOW & kWhole || at(v, MAP == kEight ? 0 : MAP == kFours ? j & 4 : j) < D; }
+  template <typename T_>
+  __device__ __forceinline__ F8 load(const T_ *row, int v) const {   // zero past the row's end
+    float f[8];
+    if (MAP == kEight) {
+      Raw8<T_> r;
+      if (on(v, 0)) r.load(row + at(v, 0));
+      else r.zero();
+      r.get(f);
+    } else if (MAP == kFours) {
+      Raw8<T_> r;
+      r.zero();
+      if (on(v, 0)) r.load4(0, row + at(v, 0));
+      if (on(v, 4)) r.load4(1, row + at(v, 4));
+      r.get(f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = on(v, j) ? to_f32(row[at(v, j)]) : 0.f;
+    }
+    return from8(f);
+  }
+  template <typename T_>
+  __device__ __forceinline__ void store(T_ *row, int v, const F8 &a) const {
+    float f[8];
+    to8(a, f);
+    if (MAP == kEight) {
+      if (on(v, 0)) store8(row + at(v, 0), f);
+    } else if (MAP == kFours) {
+      if (on(v, 0)) store4(row + at(v, 0), f[0], f[1], f[2], f[3]);
+      if (on(v, 4)) store4(row + at(v, 4), f[4], f[5], f[6], f[7]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (on(v, j)) from_f32(f[j], row + at(v, j));
+    }
+  }
+  // `a` inside the row, zero past its end
+  __device__ __forceinline__ F8 inside(const F8 &a, int v) const {
+    if (HOW & kWhole) return a;
+    if (MAP == kEight) return on(v, 0) ? a : all8(0.f);
+    float f[8];
+    to8(a, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = on(v, j) ? f[j] : 0.f;
+    return from8(f);
+  }
+  // Where the folded vectors keep a column: for consecutive eights in two planes of fours, again for the banks.
+  __device__ __forceinline__ static int kept(int c, int pieces) { return MAP == kEight ? ((c >> 2 & 1) * pieces + (c >> 3)) * 4 + (c & 3) : c; }
+  __device__ __forceinline__ F8 load_kept(const float *vec, int v, int pieces) const {
+    if (MAP != kEight) return load(vec, v);
+    float f[8];
+    const float4 a = *(const float4 *)(vec + (v * T + t) * 4), b = *(const float4 *)(vec + (pieces + v * T + t) * 4);
+    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    return from8(f);
+  }
+};
+
+// The vectors of a call, folded: in shared memory where that leaves room for the rows, else read from where they lie.
+enum { kVecW, kVecB, kVecPreW, kVecPreB };   // alpha * scale * post_weight, alpha * scale * post_bias, pre_weight, pre_bias
+struct Vectors {
+  const float *at[4];   // in shared memory
+  __device__ __forceinline__ static float value(const NormArgs &a, int which, int c) {
+    if (which == kVecPreW) return a.pre_w ? a.pre_w[c] : 1.f;
+    if (which == kVecPreB) return a.pre_b ? a.pre_b[c] : 0.f;
+    const float s = a.alpha * (a.scale ? a.scale[c] : 1.f);
+    return which == kVecW ? s * (a.post_w ? a.post_w[c] : 1.f) : a.post_b ? s * a.post_b[c] : 0.f;
+  }
+};
+// Which of them a kernel keeps; all threads, before the rows.
+template <int MAP, int V>
+__device__ __forceinline__ Vectors fold_vectors(const NormArgs &a, uint8_t *smem, bool full) {
+  Vectors vec = {{nullptr, nullptr, nullptr, nullptr}};
+  float *to = (float *)(smem + kRowsAt);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const bool used = (k < 2 ? a.flags & ALG_NORM_JOIN : a.flags & ALG_NORM_PRE) && (full || !(k & 1));
+    if (!used || !a.vectors) continue;
+    for (int c = threadIdx.x; c < a.T * V * 8; c += blockDim.x) to[Cols<MAP>::kept(c, a.T * V)] = c < a.D ? Vectors::value(a, k, c) : 0.f;
+    vec.at[k] = to;
+    to += a.T * V * 8;
+  }
+  return vec;
+}
+template <int MAP, int V, int FORM>
+__device__ __forceinline__ F8 vector8(const NormArgs &a, const Vectors &vec, int which, const Cols<MAP> &cols, int v) {
+  if (V == 1 || FORM != kAny || a.vectors) return cols.load_kept(vec.at[which], v, a.T * V);
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = cols.on(v, j) ? Vectors::value(a, which, cols.at(v, j)) : 0.f;
+  return from8(f);
+}
+
+// A row of the operands on its way into shared memory.  The warps of a group share the asking: a copy takes its thread about 150
+// cycles, and a warp that asked for all five would have the others wait at the next barrier.  (What has landed before it is expected
+// only makes the barrier's count negative for a while.)
+__device__ __forceinline__ void issue_row(const NormArgs &a, uint32_t stage, uint32_t bar, uint32_t row, int t) {
+  if (t & 31) return;
+  if (t == 0) {
+    uint32_t total = 0;
+#pragma unroll
+    for (int k = 0; k < kOps; ++k) total += a.op[k] ? a.bytes[k] : 0u;
+    tc::mbar_expect_tx(bar, total);
+  }
+  for (int k = t >> 5; k < kOps; k += a.T >> 5)
+    if (a.op[k])
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(stage + a.at[k]),
+                   "l"(a.op[k] + (uint64_t)row * a.pitch[k]), "r"(a.bytes[k]), "r"(bar)
+                   : "memory");
+}
+// Unaligned rows: the group copies them itself.
+template <typename XT, typename BT>
+__device__ __forceinline__ void copy_row(const NormArgs &a, uint8_t *stage, uint32_t row, int t) {
+#pragma unroll
+  for (int k = 0; k < kOps; ++k) {
+    if (!a.op[k]) continue;
+    const uint8_t *p = a.op[k] + (uint64_t)row * a.pitch[k];
+    for (int c = t; c < a.D; c += a.T) {
+      if (k < kN) ((XT *)(stage + a.at[k]))[c] = ((const XT *)p)[c];
+      else ((BT *)(stage + a.at[k]))[c] = ((const BT *)p)[c];
+    }
+  }
+}
+
+// The loop over a group's rows: body(row, stage, release); release() once the row's operands are read and a barrier of the group has
+// followed.
+template <int MAP, int V, typename XT, typename BT, typename Body>
+__device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vectors *vec, bool full, Body body) {
+  constexpr bool copies = MAP == kScalar;
+  const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
+  uint8_t *const rows = smem + kRowsAt + a.vectors + g * a.stages * a.stage_bytes;
+  const uint32_t bar = tc::smem_u32(smem) + g * a.stages * 8, rows_at = tc::smem_u32(rows);
+  if (!copies && t == 0) {
+    for (int s = 0; s < a.stages; ++s) tc::mbar_init(bar + 8 * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  group_barrier(g, a.T);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint32_t first = blockIdx.x * a.G + g, step = gridDim.x * a.G;
+  if (!copies)
+    for (int s = 0; s < a.stages; ++s)
+      if (first + s * step < a.M) issue_row(a, rows_at + s * a.stage_bytes, bar + 8 * s, first + s * step, t);
+  *vec = fold_vectors<MAP, V>(a, smem, full);
+  __syncthreads();
+  int s = 0;
+  uint32_t parity = 0;
+  bool failed = false;   // after a wait that ran out nothing is right, but every thread still goes the same way to the end
+  for (uint32_t row = first; row < a.M; row += step) {
+    if (copies) {
+      group_barrier(g, a.T);   // (the row before it is read)
+      copy_row<XT, BT>(a, rows, row, t);
+      group_barrier(g, a.T);
+    } else if (!tc::mbar_try_wait(bar + 8 * s, parity) && !failed) {
+      const long long t0 = clock64();
+      while (!tc::mbar_try_wait(bar + 8 * s, parity))
+        if (clock64() - t0 > a.wait_limit) {
+          failed = true;
+          atomicExch(a.status, (int)ALG_ERR_DEVICE_TIMEOUT);
+          break;
+        }
+    }
+    body(row, (const uint8_t *)rows + s * a.stage_bytes, [&] {
+      if (!copies && row + a.stages * step < a.M) issue_row(a, rows_at + s * a.stage_bytes, bar + 8 * s, row + a.stages * step, t);
+    });
+    if (!copies && ++s == a.stages) s = 0, parity ^= 1;
+  }
+}
+
+// FULL: LayerNorm, or with biases or their gradients; LayerNorm where the form is a constant.
+template <typename XT, typename BT, int MAP, int V, bool FULL, int FORM>
+__global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArgs a) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  float4 *red = (float4 *)(smem + kBarBytes);
+  const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
+  const Cols<MAP> cols = {t, a.T, a.D};
+  const float inv_d = 1.f / (float)a.D;
+  constexpr bool any = FORM == kAny;
+  constexpr int gate_of = any ? 0 : FORM / kFormGate;
+  const bool pre = any ? a.flags & ALG_NORM_PRE : FORM & kFormPre, join = any ? a.flags & ALG_NORM_JOIN : FORM & kFormJoin;
+  const bool post = any ? a.flags & ALG_NORM_POST : FORM & kFormPost, layer = any ? FULL && a.layer : FULL;
+  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of >= kGateElement;
+  const bool sig = any || gate_of == kGateRow ? a.flags & ALG_NORM_GATE_SIGMOID : gate_of == kGateSigmoid;
+  int turn = 0;
+  Vectors vec;
+  each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
+    F8 y[V], f[V], q[V];
+    bool held = true;
+    const float gate = gate_row ? to_f32(((const BT *)a.gate)[row]) : 1.f;
+    // takes the mean off z and finds 1 / sqrt(var + eps)
+    auto stat = [&](F8 (&z)[V]) {
+      if (layer) {
+        float m[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) m[0] += sum8(z[v]);
+        group_sum(m, red, turn, g, a.T);
+        if (held) release(), held = false;
+#pragma unroll
+        for (int v = 0; v < V; ++v) z[v] = cols.inside(z[v] + -m[0] * inv_d, v);
+      }
+      float s[1] = {0.f};
+#pragma unroll
+      for (int v = 0; v < V; ++v) s[0] += dot8(z[v], z[v]);
+      group_sum(s, red, turn, g, a.T);
+      if (held) release(), held = false;
+      return rsqrtf(s[0] * inv_d + a.eps);
+    };
+#pragma unroll
+    for (int v = 0; v < V; ++v) y[v] = cols.load((const XT *)(st + a.at[kX]), v);
+    if (join) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        f[v] = cols.load((const BT *)(st + a.at[kF]), v);
+        if (gate_el) q[v] = cols.load((const BT *)(st + a.at[kG]), v);
+      }
+      const float rf = post ? stat(f) : 1.f, g1 = gate_row && sig ? sigmoid(gate) : gate;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const F8 w = vector8<MAP, V, FORM>(a, vec, kVecW, cols, v);
+        F8 n = f[v] * w * rf;
+        if (FULL) n = n + vector8<MAP, V, FORM>(a, vec, kVecB, cols, v);
+        if (gate_el) {
+          if (sig) {
+            float e[8];
+            to8(q[v], e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = sigmoid(e[j]);
+            q[v] = from8(e);
+          }
+          y[v] = fma8(n, q[v], y[v]);
+        } else {
+          y[v] = fma8(n, g1, y[v]);
+        }
+        cols.store((XT *)(a.y + (uint64_t)row * a.pitch_y), v, y[v]);
+      }
+    }
+    if (pre) {
+      const float ry = stat(y);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        F8 n = y[v] * ry * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v);
+        if (FULL) n = n + vector8<MAP, V, FORM>(a, vec, kVecPreB, cols, v);
+        cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out), v, n);
+      }
+    }
+    if (held) {
+      group_barrier(g, a.T);
+      release();
+    }
+  });
+}
+
+template <typename XT, typename BT, int MAP, int V, bool FULL, int FORM>
+__global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormArgs a) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  float4 *red = (float4 *)(smem + kBarBytes);
+  const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
+  const Cols<MAP> cols = {t, a.T, a.D};
+  const float inv_d = 1.f / (float)a.D;
+  constexpr bool any = FORM == kAny;
+  constexpr int gate_of = any ? 0 : FORM / kFormGate;
+  const bool pre = any ? a.flags & ALG_NORM_PRE : FORM & kFormPre, join = any ? a.flags & ALG_NORM_JOIN : FORM & kFormJoin;
+  const bool post = any ? a.flags & ALG_NORM_POST : FORM & kFormPost, layer = any ? FULL && a.layer : FULL;
+  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of >= kGateElement;
+  const bool sig = any || gate_of == kGateRow ? a.flags & ALG_NORM_GATE_SIGMOID : gate_of == kGateSigmoid;
+  // (a form that is a constant comes with dY and with every gradient wanted)
+  const bool has_dy = any ? a.op[kT] != nullptr : true, to_f = any ? a.out != nullptr : true, to_gate = any ? a.dg != nullptr : true;
+  F8 sum[kSums][V];
+#pragma unroll
+  for (int k = 0; k < kSums; ++k)
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[k][v] = all8(0.f);
+  int turn = 0;
+  Vectors vec;
+  each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
+    // a row of eight columns a thread stays in registers, a wider one is read from its stage as needed
+    F8 hx, hn, hf;
+    auto x_of = [&](int v) { return V == 1 ? hx : cols.load((const XT *)(st + a.at[kX]), v); };
+    auto n_of = [&](int v) { return V == 1 ? hn : cols.load((const BT *)(st + a.at[kN]), v); };
+    auto f_of = [&](int v) { return V == 1 ? hf : cols.load((const BT *)(st + a.at[kF]), v); };
+    F8 d[V], q[V];   // dY, then the gradient of R; the gate
+    bool held = V == 1;
+    const float gate_1 = gate_row ? to_f32(((const BT *)a.gate)[row]) : 1.f;
+    if (V == 1) {
+      if (pre) hx = cols.load((const XT *)(st + a.at[kX]), 0), hn = cols.load((const BT *)(st + a.at[kN]), 0);
+      if (join) hf = cols.load((const BT *)(st + a.at[kF]), 0);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      d[v] = has_dy ? cols.load((const XT *)(st + a.at[kT]), v) : all8(0.f);
+      if (V == 1 && gate_el) q[v] = cols.load((const BT *)(st + a.at[kG]), v);
+    }
+    // statistics of Y and F, and the means of h = dN * pre_weight and of h times the normed Y
+    float mx = 0.f, mf = 0.f, mh = 0.f;
+    if (layer && (pre || post)) {
+      float m[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (pre) m[0] += sum8(x_of(v)), m[2] += dot8(n_of(v), vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v));
+        if (post) m[1] += sum8(f_of(v));
+      }
+      group_sum(m, red, turn, g, a.T);
+      if (held) release(), held = false;
+      mx = m[0] * inv_d, mf = m[1] * inv_d, mh = m[2] * inv_d;
+      if (V == 1) {
+        if (pre) hx = cols.inside(hx + -mx, 0);
+        if (post) hf = cols.inside(hf + -mf, 0);
+      }
+    }
+    // (x and f without their means)
+    auto xc_of = [&](int v) { return V == 1 || !layer ? x_of(v) : cols.inside(x_of(v) + -mx, v); };
+    auto fc_of = [&](int v) { return V == 1 || !layer || !post ? f_of(v) : cols.inside(f_of(v) + -mf, v); };
+    float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (pre) {
+        const F8 x = xc_of(v);
+        s[0] += dot8(x, x);
+        s[2] += dot8(x * n_of(v), vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v));
+      }
+      if (post) {
+        const F8 f = fc_of(v);
+        s[1] += dot8(f, f);
+      }
+    }
+    if (pre || post) {
+      group_sum(s, red, turn, g, a.T);
+      if (held) release(), held = false;
+    }
+    const float rx = rsqrtf(s[0] * inv_d + a.eps), rf = post ? rsqrtf(s[1] * inv_d + a.eps) : 1.f;
+    const float mhv = s[2] * inv_d * rx;
+    // the row's gate and its slope
+    const float gr = gate_row && sig ? sigmoid(gate_1) : gate_1, gs = sig ? gr * (1.f - gr) : 1.f;
+    F8 e[V];   // gradient of V
+    float m[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (pre) {
+        const F8 x = xc_of(v) * rx, n = n_of(v);
+        sum[0][v] = fma8(n, x, sum[0][v]);
+        if (FULL) sum[1][v] = sum[1][v] + n;
+        F8 h = n * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v);
+        if (layer) h = h + -mh;
+        d[v] = fma8(fma8(x, -mhv, h), rx, d[v]);
+        if (layer) d[v] = cols.inside(d[v], v);
+      }
+      cols.store((XT *)(a.y + (uint64_t)row * a.pitch_y), v, d[v]);
+      if (!join) continue;
+      const F8 f = fc_of(v) * rf, w = vector8<MAP, V, FORM>(a, vec, kVecW, cols, v);
+      F8 dg = d[v] * gr;   // the gradient behind the gate
+      F8 slope;
+      if (gate_el) {
+        F8 z = V == 1 ? q[v] : cols.load((const BT *)(st + a.at[kG]), v);
+        if (sig) {
+          float p[8];
+          to8(z, p);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = sigmoid(p[j]);
+          z = from8(p);
+          slope = fma8(z * z, -1.f, z);
+        }
+        dg = d[v] * z;
+      }
+      sum[2][v] = fma8(dg, f, sum[2][v]);
+      if (FULL) sum[3][v] = sum[3][v] + dg;
+      e[v] = dg * w;
+      if (gate_row || (gate_el && to_gate)) {
+        F8 b = f * w;
+        if (FULL) b = b + vector8<MAP, V, FORM>(a, vec, kVecB, cols, v);
+        b = b * d[v];
+        if (gate_el) {
+          if (sig) b = b * slope;
+          cols.store((BT *)(a.dg + (uint64_t)row * a.pitch_dg), v, b);
+        } else {
+          m[2] += sum8(b);
+        }
+      }
+      if (post) {
+        if (layer) m[0] += sum8(e[v]);
+        m[1] += dot8(e[v], f);
+      } else if (to_f) {
+        cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out), v, e[v]);
+      }
+    }
+    if (join && ((post && to_f) || (gate_row && to_gate))) {
+      group_sum(m, red, turn, g, a.T);
+      if (held) release(), held = false;
+      if (gate_row && to_gate && t == 0) from_f32(m[2] * gs, (BT *)a.dg + row);
+      if (post && to_f) {
+        const float me = m[0] * inv_d, mev = m[1] * inv_d;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          F8 o = fma8(fc_of(v) * rf, -mev, e[v]);
+          if (layer) o = o + -me;
+          cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out), v, o * rf);
+        }
+      }
+    }
+    if (V > 1 || held) {
+      group_barrier(g, a.T);
+      release();
+    }
+  });
+  if (!a.part) return;
+  // the groups' sums meet where the rows were, [groups][D], and are added in their order
+  float *acc = (float *)(smem + kRowsAt + a.vectors);
+  float *part = a.part + (size_t)blockIdx.x * kSums * a.D;
+#pragma unroll
+  for (int k = 0; k < kSums; ++k) {
+    if ((k < 2 ? !pre : !join) || (!FULL && (k & 1))) continue;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float f[8];
+      to8(sum[k][v], f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (cols.on(v, j)) acc[g * a.D + cols.at(v, j)] = f[j];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.D; c += blockDim.x) {
+      float s = 0.f;
+      for (int i = 0; i < a.G; ++i) s += acc[i * a.D + c];
+      part[(size_t)k * a.D + c] = s;
+    }
+  }
+}
+
+inline cudaError_t launch_norm_kernel(const void *kernel, int grid, int threads, size_t smem, cudaStream_t st, void **params) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, params);
+  if (e == cudaSuccess) count_launch(1);
+  return e;
+}
+
+constexpr int kSmemMax = kRowsAt + kBudget;
+
+template <bool BACK, typename XT, typename BT, int MAP, int V, bool FULL, int FORM>
+cudaError_t launch_rows(NormArgs &a, int grid, size_t smem, cudaStream_t st) {
+  static OncePerDevice once;
+  const void *k;
+  if constexpr (BACK) k = (const void *)norm_backward_kernel<XT, BT, MAP, V, FULL, FORM>;
+  else k = (const void *)norm_forward_kernel<XT, BT, MAP, V, FULL, FORM>;
+  const cudaError_t e = once([&] { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax); });
+  if (e != cudaSuccess) return e;
+  void *params[] = {&a};
+  return launch_norm_kernel(k, grid, a.T * a.G, smem, st, params);
+}
+
+// The kernel of a form: rows that fill the threads' pieces, or not.
+template <bool BACK, typename XT, int V, bool LAYER, int FORM>
+cudaError_t launch_form(NormArgs &a, int grid, size_t smem, cudaStream_t st) {
+  constexpr int kMap = sizeof(XT) == 4 ? kFours : kEight;
+  return a.D == a.T * V * 8 ? launch_rows<BACK, XT, __nv_bfloat16, kMap | kWhole, V, LAYER, FORM>(a, grid, smem, st)
+                            : launch_rows<BACK, XT, __nv_bfloat16, kMap, V, LAYER, FORM>(a, grid, smem, st);
+}
+template <bool BACK, typename XT, int V, bool LAYER, int BASE>
+cudaError_t launch_gate(NormArgs &a, int gate, int grid, size_t smem, cudaStream_t st) {
+  switch (gate) {
+    case kGateNone: return launch_form<BACK, XT, V, LAYER, BASE>(a, grid, smem, st);
+    case kGateRow: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateRow>(a, grid, smem, st);
+    case kGateElement: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateElement>(a, grid, smem, st);
+    default: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateSigmoid>(a, grid, smem, st);
+  }
+}
+template <bool BACK, typename XT, int V, bool LAYER>
+cudaError_t launch_forms(NormArgs &a, int form, int grid, size_t smem, cudaStream_t st) {
+  const int gate = form / kFormGate;
+  switch (form % kFormGate) {
+    case kFormJoin | kFormPost | kFormPre: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPost | kFormPre>(a, gate, grid, smem, st);
+    case kFormJoin | kFormPost: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPost>(a, gate, grid, smem, st);
+    case kFormJoin | kFormPre: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPre>(a, gate, grid, smem, st);
+    case kFormJoin: return launch_gate<BACK, XT, V, LAYER, kFormJoin>(a, gate, grid, smem, st);
+    default: return launch_form<BACK, XT, V, LAYER, kFormPre>(a, grid, smem, st);
+  }
+}
+
+}  // namespace
+}  // namespace algproj

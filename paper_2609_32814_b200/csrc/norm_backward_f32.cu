@@ -1,0 +1,10 @@
+// A block's border, backward pass, residual stream in f32: the kernels whose form is a constant.
+#include "norm.cuh"
+
+namespace algproj {
+
+cudaError_t launch_norm_backward_f32(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st) {
+  return layer ? launch_forms<true, float, 1, true>(a, form, grid, smem, st) : launch_forms<true, float, 2, false>(a, form, grid, smem, st);
+}
+
+}  // namespace algproj

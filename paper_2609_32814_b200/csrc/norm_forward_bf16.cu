@@ -1,0 +1,10 @@
+// A block's border, forward pass, residual stream in bf16: the kernels whose form is a constant.
+#include "norm.cuh"
+
+namespace algproj {
+
+cudaError_t launch_norm_forward_bf16(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st) {
+  return layer ? launch_forms<false, __nv_bfloat16, 2, true>(a, form, grid, smem, st) : launch_forms<false, __nv_bfloat16, 2, false>(a, form, grid, smem, st);
+}
+
+}  // namespace algproj
