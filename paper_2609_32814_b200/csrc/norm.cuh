@@ -105,8 +105,8 @@ __device__ __forceinline__ void group_sum(float (&v)[K], float4 *red, int &turn,
     turn ^= 1;
     if (lane < kValues) slot[mine * kValues + lane] = r;
     group_barrier(g, T);
-    r = 0.f;
-    for (int i = lane; i < warps * kValues; i += 32) r += slot[i];
+    r = lane < warps * kValues ? slot[lane] : 0.f;
+    if (kValues > 2 && lane + 32 < warps * kValues) r += slot[lane + 32];   // (sixteen warps at most)
 #pragma unroll
     for (int o = kValues; o < 32; o <<= 1) r += __shfl_xor_sync(~0u, r, o);
   } else {
@@ -195,6 +195,12 @@ struct Vectors {
     const float s = a.alpha * (a.scale ? a.scale[c] : 1.f);
     return which == kVecW ? s * (a.post_w ? a.post_w[c] : 1.f) : a.post_b ? s * a.post_b[c] : 0.f;
   }
+  __device__ __forceinline__ static float4 value4(const NormArgs &a, int which, int c) {
+    auto four = [&](const float *p, float none) { return p ? *(const float4 *)(p + c) : make_float4(none, none, none, none); };
+    if (which >= kVecPreW) return which == kVecPreW ? four(a.pre_w, 1.f) : four(a.pre_b, 0.f);
+    const float4 s = four(a.scale, 1.f), v = which == kVecW ? four(a.post_w, 1.f) : four(a.post_b, 0.f);
+    return make_float4(a.alpha * s.x * v.x, a.alpha * s.y * v.y, a.alpha * s.z * v.z, a.alpha * s.w * v.w);
+  }
 };
 // Which of them a kernel keeps; all threads, before the rows.
 template <int MAP, int V>
@@ -205,7 +211,13 @@ __device__ __forceinline__ Vectors fold_vectors(const NormArgs &a, uint8_t *smem
   for (int k = 0; k < 4; ++k) {
     const bool used = (k < 2 ? a.flags & ALG_NORM_JOIN : a.flags & ALG_NORM_PRE) && (full || !(k & 1));
     if (!used || !a.vectors) continue;
-    for (int c = threadIdx.x; c < a.T * V * 8; c += blockDim.x) to[Cols<MAP>::kept(c, a.T * V)] = c < a.D ? Vectors::value(a, k, c) : 0.f;
+    if (Cols<MAP>::MAP == kScalar) {
+      for (int c = threadIdx.x; c < a.T * V * 8; c += blockDim.x) to[c] = c < a.D ? Vectors::value(a, k, c) : 0.f;
+    } else {   // (D is a multiple of eight, and the vectors lie on 16 bytes)
+#pragma unroll 4
+      for (int c = threadIdx.x * 4; c < a.T * V * 8; c += blockDim.x * 4)
+        *(float4 *)(to + Cols<MAP>::kept(c, a.T * V)) = c < a.D ? Vectors::value4(a, k, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
     vec.at[k] = to;
     to += a.T * V * 8;
   }
@@ -296,6 +308,15 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
   }
 }
 
+// The gate of a row, asked for one row ahead.
+template <typename BT>
+__device__ __forceinline__ float next_gate(const BT *gate, uint32_t row, const NormArgs &a, float &ahead) {
+  const uint32_t step = gridDim.x * a.G;
+  const float now = row < step ? to_f32(gate[row]) : ahead;   // (a group's first row is below the step)
+  if (row + step < a.M) ahead = to_f32(gate[row + step]);
+  return now;
+}
+
 // FULL: LayerNorm, or with biases or their gradients; LayerNorm where the form is a constant.
 template <typename XT, typename BT, int MAP, int V, bool FULL, int FORM>
 __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArgs a) {
@@ -312,10 +333,11 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArg
   const bool sig = any || gate_of == kGateRow ? a.flags & ALG_NORM_GATE_SIGMOID : gate_of == kGateSigmoid;
   int turn = 0;
   Vectors vec;
+  float gate_ahead = 0.f;
   each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
     F8 y[V], f[V], q[V];
     bool held = true;
-    const float gate = gate_row ? to_f32(((const BT *)a.gate)[row]) : 1.f;
+    const float gate = gate_row ? next_gate((const BT *)a.gate, row, a, gate_ahead) : 1.f;
     // takes the mean off z and finds 1 / sqrt(var + eps)
     auto stat = [&](F8 (&z)[V]) {
       if (layer) {
@@ -401,17 +423,19 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
     for (int v = 0; v < V; ++v) sum[k][v] = all8(0.f);
   int turn = 0;
   Vectors vec;
+  float gate_ahead = 0.f;
   each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
     // a row of eight columns a thread stays in registers, a wider one is read from its stage as needed
-    F8 hx, hn, hf;
+    F8 hx, hn, hf, hh;   // (hh: dN * pre_weight)
     auto x_of = [&](int v) { return V == 1 ? hx : cols.load((const XT *)(st + a.at[kX]), v); };
     auto n_of = [&](int v) { return V == 1 ? hn : cols.load((const BT *)(st + a.at[kN]), v); };
+    auto h_of = [&](int v) { return V == 1 ? hh : n_of(v) * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v); };
     auto f_of = [&](int v) { return V == 1 ? hf : cols.load((const BT *)(st + a.at[kF]), v); };
     F8 d[V], q[V];   // dY, then the gradient of R; the gate
     bool held = V == 1;
-    const float gate_1 = gate_row ? to_f32(((const BT *)a.gate)[row]) : 1.f;
+    const float gate_1 = gate_row ? next_gate((const BT *)a.gate, row, a, gate_ahead) : 1.f;
     if (V == 1) {
-      if (pre) hx = cols.load((const XT *)(st + a.at[kX]), 0), hn = cols.load((const BT *)(st + a.at[kN]), 0);
+      if (pre) hx = cols.load((const XT *)(st + a.at[kX]), 0), hn = cols.load((const BT *)(st + a.at[kN]), 0), hh = hn * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, 0);
       if (join) hf = cols.load((const BT *)(st + a.at[kF]), 0);
     }
 #pragma unroll
@@ -425,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
       float m[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        if (pre) m[0] += sum8(x_of(v)), m[2] += dot8(n_of(v), vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v));
+        if (pre) m[0] += sum8(x_of(v)), m[2] += sum8(h_of(v));
         if (post) m[1] += sum8(f_of(v));
       }
       group_sum(m, red, turn, g, a.T);
@@ -445,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
       if (pre) {
         const F8 x = xc_of(v);
         s[0] += dot8(x, x);
-        s[2] += dot8(x * n_of(v), vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v));
+        s[2] += dot8(x, h_of(v));
       }
       if (post) {
         const F8 f = fc_of(v);
@@ -468,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
         const F8 x = xc_of(v) * rx, n = n_of(v);
         sum[0][v] = fma8(n, x, sum[0][v]);
         if (FULL) sum[1][v] = sum[1][v] + n;
-        F8 h = n * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v);
+        F8 h = h_of(v);
         if (layer) h = h + -mh;
         d[v] = fma8(fma8(x, -mhv, h), rx, d[v]);
         if (layer) d[v] = cols.inside(d[v], v);
