@@ -455,6 +455,7 @@ alg_status_t alg_norm_last_status(alg_norm_t h, void *stream, alg_status_t *stat
  * largest magnitude fits the format (448 for E4M3, 127 for INT8), at least 2^-120, so the codes are exact functions of the
  * values: a value is off by at most 2^-4 of itself (E4M3, above the format's subnormals) or half a step of its
  * block (INT8).  A block that holds an infinity or a NaN has s = 255 and reads back as NaN.
+ * (Magnitudes within half a step of 2^128 read back as infinite.)
  *   store / load     X (M x cols, x_dtype, ungated handles) to records and back
  *   act_forward      A = act(Z), ungated, Z M x cols; or A = act(G) .* U with Z = [G | U] M x 2 cols, gated.  Writes the
  *                    record of Z beside A in the same pass; ckpt == NULL keeps nothing.

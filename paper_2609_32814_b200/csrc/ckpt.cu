@@ -46,8 +46,23 @@ struct CkptArgs {
   int int8;
 };
 
-// Codes of eight values whose block's largest magnitude has the bits `top`; the scale byte.
-__device__ __forceinline__ uint2 encode8(const float (&f)[8], uint32_t top, int int8, int *scale) {
+// The largest magnitude of eight values, as bits: one that is not finite is above all others.
+__device__ __forceinline__ uint32_t largest8(const Raw8<__nv_bfloat16> &r) {
+  const uint32_t m = 0x7FFF7FFFu;
+  const uint32_t v = __vmaxu2(__vmaxu2(r.a.x & m, r.a.y & m), __vmaxu2(r.a.z & m, r.a.w & m));
+  return max(v << 16, v & 0x7FFF0000u);
+}
+__device__ __forceinline__ uint32_t largest8(const Raw8<float> &r) {
+  auto most = [](float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return d;
+  };
+  return __float_as_uint(most(most(most(r.a.x, r.a.y), most(r.a.z, r.a.w)), most(most(r.b.x, r.b.y), most(r.b.z, r.b.w))));
+}
+// Codes of eight values whose block's largest magnitude has the bits `top`; the scale byte.  Integers without a conversion: x * 2^-e plus
+// 1.5 * 2^23 is rounded to a whole number, whose low byte is the code; back the same way from 2^23 + 128 + code, exactly.
+__device__ __forceinline__ uint2 encode8(const F8 &x, uint32_t top, int int8, int *scale) {
   if (top >= 0x7F800000u) {   // an infinity or a NaN
     *scale = 255;
     return make_uint2(0u, 0u);
@@ -56,61 +71,105 @@ __device__ __forceinline__ uint2 encode8(const float (&f)[8], uint32_t top, int 
   const int e = max(kMinExp, (int)((top + (int8 ? 0x7FFFFFu - 0x7E0000u : 0x7FFFFFu - 0x600000u)) >> 23) - 127 - (int8 ? 6 : 8));
   *scale = e + 127;
   const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-  uint32_t w[2];
+  float f[8];
   if (int8) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t v = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v |= ((uint32_t)__float2int_rn(f[4 * h + j] * inv) & 255u) << (8 * j);
-      w[h] = v;
-    }
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * h] * inv, f[4 * h + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * h + 2] * inv, f[4 * h + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-      w[h] = lo | hi << 16;
-    }
+    to8(fma8(x, inv, all8(12582912.f)), f);
+    auto pack = [](float a, float b, float c, float d) {
+      return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+    };
+    return make_uint2(pack(f[0], f[1], f[2], f[3]), pack(f[4], f[5], f[6], f[7]));
   }
-  return make_uint2(w[0], w[1]);
+  to8(x * inv, f);
+  auto pack = [](float a, float b, float c, float d) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    return lo | (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
+  };
+  return make_uint2(pack(f[0], f[1], f[2], f[3]), pack(f[4], f[5], f[6], f[7]));
 }
-__device__ __forceinline__ void decode8(uint2 c, int s, int int8, float (&f)[8]) {
+__device__ __forceinline__ F8 decode8(uint2 c, int s, int int8) {
   const float scale = s == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)s << 23);
-  const uint32_t w[2] = {c.x, c.y};
+  float f[8];
   if (int8) {
+    const uint32_t lo = c.x ^ 0x80808080u, hi = c.y ^ 0x80808080u;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = (float)(int8_t)(w[j >> 2] >> (8 * (j & 3)) & 255u) * scale;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j >> 1] >> (16 * (j & 1)) & 0xFFFFu), __NV_E4M3);
-      const float2 v = __half22float2(*(const __half2 *)&h);
-      f[2 * j] = v.x * scale, f[2 * j + 1] = v.y * scale;
-    }
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(__byte_perm(j < 4 ? lo : hi, 0x4B000000u, 0x7440 | (j & 3)));
+    return (from8(f) + -8388736.f) * scale;
   }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((j < 2 ? c.x : c.y) >> (16 * (j & 1)) & 0xFFFFu), __NV_E4M3);
+    const float2 v = __half22float2(*(const __half2 *)&h);
+    f[2 * j] = v.x, f[2 * j + 1] = v.y;
+  }
+  return from8(f) * scale;
 }
 
-// act(z), and its derivative.
-template <int ACT>
-__device__ __forceinline__ float act1(float z, float *slope) {
+__device__ __forceinline__ F8 each(const F8 &x, float (*g)(float)) {
+  float f[8];
+  to8(x, f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = g(f[j]);
+  return from8(f);
+}
+__device__ __forceinline__ float exp2_(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ F8 minus(const F8 &a) { return a * -1.f; }
+
+// act(z), and its derivative where `slope` is not null.
+template <typename T, int ACT>
+__device__ __forceinline__ F8 act8(const F8 &z, F8 *slope) {
+  const float log2e = 1.4426950408889634f;
   if (ACT == ALG_ACT_SILU) {
-    const float p = __fdividef(1.f, 1.f + __expf(-z));
-    *slope = p * fmaf(z, 1.f - p, 1.f);
-    return z * p;
+    const F8 p = each(each(z * -log2e, exp2_) + 1.f, reciprocal), a = z * p;
+    if (slope) *slope = fma8(a, minus(p) + 1.f, p);
+    return a;
+  }
+  if (ACT == ALG_ACT_GELU_TANH) {   // (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), 2u = 2k z (1 + c z^2)
+    const float k2 = 2.f * 0.7978845608028654f, c = 0.044715f;
+    const F8 zz = z * z, p = each(each(z * fma8(zz, -log2e * k2 * c, all8(-log2e * k2)), exp2_) + 1.f, reciprocal), a = z * p;
+    if (slope) *slope = fma8(a * (minus(p) + 1.f), fma8(zz, 3.f * k2 * c, all8(k2)), p);
+    return a;
   }
   if (ACT == ALG_ACT_GELU_ERF) {
-    const float p = fmaf(0.5f, erff(z * 0.70710678118654752f), 0.5f);
-    *slope = fmaf(z * 0.39894228040143268f, __expf(-0.5f * z * z), p);
-    return z * p;
+    float f[8], t[8], d[8];
+    to8(z, f);
+    if (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = fmaf(0.5f, erff(f[j] * 0.70710678118654752f), 0.5f);
+      const F8 p = from8(t);
+      if (slope) *slope = fma8(z * 0.39894228040143268f, each(z * z * (-0.5f * log2e), exp2_), p);
+      return z * p;
+    }
+    // bf16 results: the lower tail 2^p(|z|) of the projection kernels' epilogues, off by 2.4e-6 at most
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = fminf(fabsf(f[j]), 6.f), d[j] = fabsf(f[j]), f[j] = fmaxf(f[j], 0.f);
+    const F8 u = from8(t);
+    F8 q = fma8(u, all8(3.3093889e-05f), all8(-7.6922908e-04f));
+    q = fma8(q, u, all8(8.0807470e-03f));
+    q = fma8(q, u, all8(-5.3412151e-02f));
+    q = fma8(q, u, all8(-4.5877093e-01f));
+    q = fma8(q, u, all8(-1.1512017f));
+    q = fma8(q, u, all8(-0.99999309f));
+    const F8 tail = each(q, exp2_), a = fma8(minus(from8(d)), tail, from8(f));
+    if (slope) {
+      float h[8], zf[8];
+      to8(minus(tail) + 0.5f, h);
+      to8(z, zf);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = copysignf(h[j], zf[j]);
+      *slope = fma8(z * 0.39894228040143268f, each(z * z * (-0.5f * log2e), exp2_), from8(h) + 0.5f);
+    }
+    return a;
   }
-  if (ACT == ALG_ACT_GELU_TANH) {   // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
-    const float z2 = z * z;
-    const float p = __fdividef(1.f, 1.f + __expf(-2.f * 0.7978845608028654f * z * fmaf(0.044715f, z2, 1.f)));
-    *slope = fmaf(2.f * 0.7978845608028654f * z * fmaf(3.f * 0.044715f, z2, 1.f), p * (1.f - p), p);
-    return z * p;
-  }
-  *slope = 1.f;
+  if (slope) *slope = all8(1.f);
   return z;
 }
 
@@ -128,7 +187,9 @@ __device__ __forceinline__ void fetch8(Raw8<T> &r, const T *row, int c, int cols
   }
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void put8(T *row, int c, int cols, const float (&f)[8]) {
+__device__ __forceinline__ void put8(T *row, int c, int cols, const F8 &a) {
+  float f[8];
+  to8(a, f);
   if (VEC) {
     if (c < cols) store8(row + c, f);
   } else {
@@ -139,14 +200,13 @@ __device__ __forceinline__ void put8(T *row, int c, int cols, const float (&f)[8
 }
 
 // Whole warps call this: the maximum of a block is found among its four threads.
-__device__ __forceinline__ void keep8(const float (&f)[8], uint8_t *codes, uint8_t *scale, bool on, int int8) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+template <typename T>
+__device__ __forceinline__ void keep8(const Raw8<T> &r, const F8 &x, uint8_t *codes, uint8_t *scale, bool on, int int8) {
+  uint32_t top = largest8(r);
   top = max(top, __shfl_xor_sync(~0u, top, 1));
   top = max(top, __shfl_xor_sync(~0u, top, 2));
   int s;
-  const uint2 w = encode8(f, top, int8, &s);
+  const uint2 w = encode8(x, top, int8, &s);
   if (!on) return;
   *(uint2 *)codes = w;
   if ((threadIdx.x & 3) == 0) *scale = (uint8_t)s;
@@ -167,23 +227,27 @@ __global__ void __launch_bounds__(kThreads) ckpt_kernel(const CkptArgs a) {
       const int u = on ? i - r * a.units : 0, c = u * 8;
       uint8_t *rec = a.ckpt + b * a.row_bytes;
       const int limit = on ? a.cols : 0;
-      float z[8], g2[8];
+      auto eight = [](const Raw8<T> &r) {
+        float f[8];
+        r.get(f);
+        return from8(f);
+      };
       if (OP == kStore || OP == kForward) {
         const T *row = (const T *)a.in + b * a.ld_in;
         Raw8<T> raw, raw2;
         fetch8<T, VEC>(raw, row, c, limit);
         if (GATED) fetch8<T, VEC>(raw2, row + a.cols, c, limit);
-        raw.get(z);
-        if (GATED) raw2.get(g2);
+        const F8 z = eight(raw);
+        F8 up;
+        if (GATED) up = eight(raw2);
         if (OP == kForward) {
-          float f[8], slope;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = act1<ACT>(z[j], &slope) * (GATED ? g2[j] : 1.f);
+          F8 f = act8<T, ACT>(z, nullptr);
+          if (GATED) f = f * up;
           put8<T, VEC>((T *)a.out + b * a.ld_out, c, limit, f);
         }
         if (OP == kStore || a.ckpt) {
-          keep8(z, rec + c, rec + codes + (u >> 2), on, a.int8);
-          if (GATED) keep8(g2, rec + a.padded + c, rec + codes + (a.padded >> 5) + (u >> 2), on, a.int8);
+          keep8(raw, z, rec + c, rec + codes + (u >> 2), on, a.int8);
+          if (GATED) keep8(raw2, up, rec + a.padded + c, rec + codes + (a.padded >> 5) + (u >> 2), on, a.int8);
         }
       } else if (on) {
         const uint2 w = *(const uint2 *)(rec + c);
@@ -192,26 +256,19 @@ __global__ void __launch_bounds__(kThreads) ckpt_kernel(const CkptArgs a) {
         int s2;
         if (GATED) w2 = *(const uint2 *)(rec + a.padded + c), s2 = rec[codes + (a.padded >> 5) + (u >> 2)];
         if (OP == kLoad) {
-          decode8(w, s, a.int8, z);
-          put8<T, VEC>((T *)a.out + b * a.ld_out, c, limit, z);
+          put8<T, VEC>((T *)a.out + b * a.ld_out, c, limit, decode8(w, s, a.int8));
         } else {
           Raw8<T> raw;
-          float d[8], dz[8], du[8], f[8];
           fetch8<T, VEC>(raw, (const T *)a.in + b * a.ld_in, c, limit);
-          decode8(w, s, a.int8, z);
-          if (GATED) decode8(w2, s2, a.int8, g2);
-          raw.get(d);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float slope;
-            const float v = act1<ACT>(z[j], &slope), up = GATED ? g2[j] : 1.f;
-            dz[j] = slope * up * d[j];
-            du[j] = v * d[j];
-            f[j] = v * up;
-          }
+          const F8 z = decode8(w, s, a.int8), d = eight(raw);
+          F8 slope, f = act8<T, ACT>(z, &slope);
           T *out = (T *)a.out + b * a.ld_out;
-          put8<T, VEC>(out, c, limit, dz);
-          if (GATED) put8<T, VEC>(out + a.cols, c, limit, du);
+          if (GATED) {
+            const F8 up = decode8(w2, s2, a.int8);
+            put8<T, VEC>(out + a.cols, c, limit, f * d);
+            slope = slope * up, f = f * up;
+          }
+          put8<T, VEC>(out, c, limit, slope * d);
           if (a.again) put8<T, VEC>((T *)a.again + b * a.ld_again, c, limit, f);
         }
       }

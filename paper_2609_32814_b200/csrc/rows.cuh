@@ -61,8 +61,14 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, float a, float b, float
 }
 __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *(float4 *)p = make_float4(a, b, c, d); }
 __device__ __forceinline__ void store8(float *p, const float (&f)[8]) {
-  ((float4 *)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-  ((float4 *)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  if (((uintptr_t)p & 31u) == 0) {   // whole sectors: 16 bytes and 16 more would write each twice
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]),
+                 "f"(f[7])
+                 : "memory");
+  } else {
+    ((float4 *)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    ((float4 *)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  }
 }
 
 // Eight values as four pairs, for the packed fp32 instructions: half as many issue slots as one value at a time.
