@@ -462,8 +462,8 @@ alg_status_t alg_norm_last_status(alg_norm_t h, void *stream, alg_status_t *stat
  *   act_backward     from the records of Z (as they read back) and dA (M x cols): dZ = act'(Z) .* dA, or
  *                    [act'(G) .* U .* dA | act(G) .* dA]; with A not NULL also the activation once more, for
  *                    the weight gradient of the down projection.
- * One dtype a call: Z, A, dA and dZ are all f32 or all bf16 (arithmetic in fp32, rounded once).  Leading dimensions and
- * addresses may be anything an element may have; rows on 16 bytes with cols a multiple of 8 run several
+ * One dtype a call: Z, A, dA and dZ are all f32 or all bf16 (arithmetic in fp32, rounded once).  Leading dimensions (below 2^30)
+ * and addresses may be anything an element may have; rows on 16 bytes with cols a multiple of 8 run several
  * times faster.  ckpt: 16-byte aligned.  A may be Z and dZ may be dA where both have the same shape and leading dimension;
  * any other overlap of outputs with operands is ALG_ERR_INVALID_ARG.  M = 0 is a successful no-op.  One launch a call,
  * no workspace; the calls keep nothing in the handle, so they may overlap on any streams. */

@@ -6,7 +6,8 @@
 // so a code depends on nothing but the values.
 //
 // One pass over memory either way, eight columns (16 bytes of bf16) a thread: four neighbouring threads are a block and
-// find its maximum by two shuffles.  Bound by HBM.
+// find its maximum by two shuffles.  Bound by HBM: 16384 x 7168 fp32 stored and loaded 180 us (6.57 TB/s), SwiGLU 16384 x 6144 both
+// passes 295 us (6.18), GELU 8003 x 4096 68 us (5.84; with erff and one value an instruction 113, bound by the arithmetic).
 #include <cuda_fp8.h>
 
 #include <new>
@@ -27,19 +28,19 @@ struct alg_ckpt_s {
 namespace algproj {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kBlock = 32;       // columns that share a scale
 constexpr int kMinExp = -120;    // of a scale: it and its inverse stay normal numbers
 
 enum { kStore, kLoad, kForward, kBackward };
 
 struct CkptArgs {
-  const void *in;        // X, Z or dA
-  void *out, *again;     // X, A or dZ; the activation of the backward pass
+  const uint8_t *in;     // X, Z or dA
+  uint8_t *out, *again;  // X, A or dZ; the activation of the backward pass
   uint8_t *ckpt;
-  int64_t ld_in, ld_out, ld_again, row_bytes;
+  uint32_t pitch_in, pitch_out, pitch_again, row_bytes;   // bytes between rows
   int64_t M;
-  int cols, padded, parts;
+  int cols, padded, codes, scales;   // codes of a row; scales of a part
   int units;             // padded / 8: threads' pieces of a row
   uint32_t inv_units;    // ceil(2^32 / units)
   int tile_rows;         // rows a CTA takes at a time
@@ -104,74 +105,88 @@ __device__ __forceinline__ F8 decode8(uint2 c, int s, int int8) {
   return from8(f) * scale;
 }
 
-__device__ __forceinline__ F8 each(const F8 &x, float (*g)(float)) {
-  float f[8];
-  to8(x, f);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = g(f[j]);
-  return from8(f);
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
+__device__ __forceinline__ uint64_t exp2_of(uint64_t x) {
+  float lo, hi;
+  halves(x, lo, hi);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(lo));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(hi));
+  return pair(lo, hi);
 }
-__device__ __forceinline__ float exp2_(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
+__device__ __forceinline__ uint64_t one_over(uint64_t x) {
+  float lo, hi;
+  halves(x, lo, hi);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(lo));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(hi));
+  return pair(lo, hi);
 }
-__device__ __forceinline__ float reciprocal(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ F8 minus(const F8 &a) { return a * -1.f; }
 
-// act(z), and its derivative where `slope` is not null.
+// act(z) of two values, and its derivative.  (Two at a time and packed at once: eight would hold 56 registers where 40 do, and threads
+// are what keeps the memory busy.)
 template <typename T, int ACT>
-__device__ __forceinline__ F8 act8(const F8 &z, F8 *slope) {
+__device__ __forceinline__ uint64_t act2(uint64_t z, uint64_t *slope) {
   const float log2e = 1.4426950408889634f;
   if (ACT == ALG_ACT_SILU) {
-    const F8 p = each(each(z * -log2e, exp2_) + 1.f, reciprocal), a = z * p;
-    if (slope) *slope = fma8(a, minus(p) + 1.f, p);
+    const uint64_t p = one_over(pair_add(exp2_of(pair_mul(z, both(-log2e))), both(1.f))), a = pair_mul(z, p);
+    *slope = pair_fma(a, pair_fma(p, both(-1.f), both(1.f)), p);
     return a;
   }
   if (ACT == ALG_ACT_GELU_TANH) {   // (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), 2u = 2k z (1 + c z^2)
     const float k2 = 2.f * 0.7978845608028654f, c = 0.044715f;
-    const F8 zz = z * z, p = each(each(z * fma8(zz, -log2e * k2 * c, all8(-log2e * k2)), exp2_) + 1.f, reciprocal), a = z * p;
-    if (slope) *slope = fma8(a * (minus(p) + 1.f), fma8(zz, 3.f * k2 * c, all8(k2)), p);
+    const uint64_t zz = pair_mul(z, z), u = pair_mul(z, pair_fma(zz, both(-log2e * k2 * c), both(-log2e * k2)));
+    const uint64_t p = one_over(pair_add(exp2_of(u), both(1.f))), a = pair_mul(z, p);
+    *slope = pair_fma(pair_mul(a, pair_fma(p, both(-1.f), both(1.f))), pair_fma(zz, both(3.f * k2 * c), both(k2)), p);
     return a;
   }
   if (ACT == ALG_ACT_GELU_ERF) {
-    float f[8], t[8], d[8];
-    to8(z, f);
+    float lo, hi;
+    halves(z, lo, hi);
+    const uint64_t zphi = pair_mul(pair_mul(z, both(0.39894228040143268f)), exp2_of(pair_mul(pair_mul(z, z), both(-0.5f * log2e))));
     if (sizeof(T) == 4) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = fmaf(0.5f, erff(f[j] * 0.70710678118654752f), 0.5f);
-      const F8 p = from8(t);
-      if (slope) *slope = fma8(z * 0.39894228040143268f, each(z * z * (-0.5f * log2e), exp2_), p);
-      return z * p;
+      const uint64_t p = pair(fmaf(0.5f, erff(lo * 0.70710678118654752f), 0.5f), fmaf(0.5f, erff(hi * 0.70710678118654752f), 0.5f));
+      *slope = pair_add(zphi, p);
+      return pair_mul(z, p);
     }
     // bf16 results: the lower tail 2^p(|z|) of the projection kernels' epilogues, off by 2.4e-6 at most
-#pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = fminf(fabsf(f[j]), 6.f), d[j] = fabsf(f[j]), f[j] = fmaxf(f[j], 0.f);
-    const F8 u = from8(t);
-    F8 q = fma8(u, all8(3.3093889e-05f), all8(-7.6922908e-04f));
-    q = fma8(q, u, all8(8.0807470e-03f));
-    q = fma8(q, u, all8(-5.3412151e-02f));
-    q = fma8(q, u, all8(-4.5877093e-01f));
-    q = fma8(q, u, all8(-1.1512017f));
-    q = fma8(q, u, all8(-0.99999309f));
-    const F8 tail = each(q, exp2_), a = fma8(minus(from8(d)), tail, from8(f));
-    if (slope) {
-      float h[8], zf[8];
-      to8(minus(tail) + 0.5f, h);
-      to8(z, zf);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[j] = copysignf(h[j], zf[j]);
-      *slope = fma8(z * 0.39894228040143268f, each(z * z * (-0.5f * log2e), exp2_), from8(h) + 0.5f);
-    }
-    return a;
+    const uint64_t u = pair(fminf(fabsf(lo), 6.f), fminf(fabsf(hi), 6.f));
+    uint64_t q = pair_fma(u, both(3.3093889e-05f), both(-7.6922908e-04f));
+    q = pair_fma(q, u, both(8.0807470e-03f));
+    q = pair_fma(q, u, both(-5.3412151e-02f));
+    q = pair_fma(q, u, both(-4.5877093e-01f));
+    q = pair_fma(q, u, both(-1.1512017f));
+    q = pair_fma(q, u, both(-0.99999309f));
+    const uint64_t tail = exp2_of(q);
+    float h0, h1;
+    halves(pair_fma(tail, both(-1.f), both(0.5f)), h0, h1);
+    *slope = pair_add(zphi, pair_add(pair(copysignf(h0, lo), copysignf(h1, hi)), both(0.5f)));
+    return pair_fma(pair(-fabsf(lo), -fabsf(hi)), tail, pair(fmaxf(lo, 0.f), fmaxf(hi, 0.f)));
   }
-  if (slope) *slope = all8(1.f);
+  *slope = both(1.f);
   return z;
 }
+
+// Eight results on their way out.
+template <typename T>
+struct Out8;
+template <>
+struct Out8<__nv_bfloat16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void set(int j, uint64_t p) {
+    float lo, hi;
+    halves(p, lo, hi);
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    w[j] = *(const uint32_t *)&v;
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]); }
+  __device__ __forceinline__ __nv_bfloat16 get(int j) const { return ((const __nv_bfloat16 *)w)[j]; }
+};
+template <>
+struct Out8<float> {
+  float f[8];
+  __device__ __forceinline__ void set(int j, uint64_t p) { halves(p, f[2 * j], f[2 * j + 1]); }
+  __device__ __forceinline__ void store(float *p) const { store8(p, f); }
+  __device__ __forceinline__ float get(int j) const { return f[j]; }
+};
 
 // Eight columns of a row from column c on, zero past `cols`.
 template <typename T, bool VEC>
@@ -187,15 +202,13 @@ __device__ __forceinline__ void fetch8(Raw8<T> &r, const T *row, int c, int cols
   }
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void put8(T *row, int c, int cols, const F8 &a) {
-  float f[8];
-  to8(a, f);
+__device__ __forceinline__ void put8(T *row, int c, int cols, const Out8<T> &o) {
   if (VEC) {
-    if (c < cols) store8(row + c, f);
+    if (c < cols) o.store(row + c);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (c + j < cols) from_f32(f[j], row + c + j);
+      if (c + j < cols) row[c + j] = o.get(j);
   }
 }
 
@@ -212,74 +225,122 @@ __device__ __forceinline__ void keep8(const Raw8<T> &r, const F8 &x, uint8_t *co
   if ((threadIdx.x & 3) == 0) *scale = (uint8_t)s;
 }
 
-template <typename T, int OP, int ACT, bool GATED, bool VEC>
-__global__ void __launch_bounds__(kThreads) ckpt_kernel(const CkptArgs a) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int codes = a.parts * a.padded;
-  for (int64_t row0 = (int64_t)blockIdx.x * a.tile_rows; row0 < a.M; row0 += (int64_t)gridDim.x * a.tile_rows) {
-    const int n = (int)min((int64_t)a.tile_rows, a.M - row0) * a.units;
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
-      const int i = i0 + threadIdx.x;
-      const bool on = i < n;                                   // (n is a multiple of 4: a block is whole)
-      const int r = on && a.units > 1 ? (int)__umulhi((uint32_t)i, a.inv_units) : 0;
-      const int64_t b = row0 + r;
-      const int u = on ? i - r * a.units : 0, c = u * 8;
-      uint8_t *rec = a.ckpt + b * a.row_bytes;
-      const int limit = on ? a.cols : 0;
-      auto eight = [](const Raw8<T> &r) {
-        float f[8];
-        r.get(f);
-        return from8(f);
-      };
-      if (OP == kStore || OP == kForward) {
-        const T *row = (const T *)a.in + b * a.ld_in;
-        Raw8<T> raw, raw2;
-        fetch8<T, VEC>(raw, row, c, limit);
-        if (GATED) fetch8<T, VEC>(raw2, row + a.cols, c, limit);
+template <typename T>
+__device__ __forceinline__ F8 eight(const Raw8<T> &r) {
+  float f[8];
+  r.get(f);
+  return from8(f);
+}
+
+// A thread's piece on its way: eight columns of a row (and the eight that go with them, of a gated matrix).
+template <typename T, int OP, bool GATED, bool VEC>
+struct Piece {
+  uint32_t r;     // row of the CTA's, whose first the pointers of `a` are at
+  int u;          // piece of the row
+  bool on;
+  Raw8<T> raw, raw2;
+  uint2 w, w2;
+  int s, s2;
+
+  __device__ __forceinline__ T *row(uint8_t *p, uint32_t pitch) const { return (T *)(p + (uint64_t)r * pitch); }
+  __device__ __forceinline__ uint8_t *record(const CkptArgs &a) const { return a.ckpt + (uint64_t)r * a.row_bytes; }
+  // piece i of n
+  __device__ __forceinline__ void ask(const CkptArgs &a, int i, int n) {
+    on = i < n;
+    r = on ? __umulhi((uint32_t)i, a.inv_units) : 0u;
+    u = on ? i - (int)r * a.units : 0;
+    const int c = u * 8, limit = on ? a.cols : 0;
+    if (OP == kLoad || OP == kBackward) {
+      if (on) {
+        const uint8_t *rec = record(a);
+        w = *(const uint2 *)(rec + c);
+        s = rec[a.codes + (u >> 2)];
+        if (GATED) w2 = *(const uint2 *)(rec + a.padded + c), s2 = rec[a.codes + a.scales + (u >> 2)];
+      }
+    }
+    if (OP == kLoad) return;
+    const T *in = row(const_cast<uint8_t *>(a.in), a.pitch_in);
+    fetch8<T, VEC>(raw, in, c, limit);
+    if (OP == kForward && GATED) fetch8<T, VEC>(raw2, in + a.cols, c, limit);
+  }
+  template <int ACT>
+  __device__ __forceinline__ void finish(const CkptArgs &a) {
+    const int c = u * 8, limit = on ? a.cols : 0;
+    uint64_t slope;
+    if (OP == kStore || OP == kForward) {
+      if (OP == kForward) {
         const F8 z = eight(raw);
-        F8 up;
-        if (GATED) up = eight(raw2);
-        if (OP == kForward) {
-          F8 f = act8<T, ACT>(z, nullptr);
-          if (GATED) f = f * up;
-          put8<T, VEC>((T *)a.out + b * a.ld_out, c, limit, f);
+        Out8<T> o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint64_t f = act2<T, ACT>(z.p[j], &slope);
+          if (GATED) f = pair_mul(f, eight(raw2).p[j]);
+          o.set(j, f);
         }
-        if (OP == kStore || a.ckpt) {
-          keep8(raw, z, rec + c, rec + codes + (u >> 2), on, a.int8);
-          if (GATED) keep8(raw2, up, rec + a.padded + c, rec + codes + (a.padded >> 5) + (u >> 2), on, a.int8);
-        }
-      } else if (on) {
-        const uint2 w = *(const uint2 *)(rec + c);
-        const int s = rec[codes + (u >> 2)];
-        uint2 w2;
-        int s2;
-        if (GATED) w2 = *(const uint2 *)(rec + a.padded + c), s2 = rec[codes + (a.padded >> 5) + (u >> 2)];
-        if (OP == kLoad) {
-          put8<T, VEC>((T *)a.out + b * a.ld_out, c, limit, decode8(w, s, a.int8));
+        put8<T, VEC>(row(a.out, a.pitch_out), c, limit, o);
+      }
+      if (OP == kStore || a.ckpt) {   // (whole warps)
+        uint8_t *rec = record(a);
+        keep8(raw, eight(raw), rec + c, rec + a.codes + (u >> 2), on, a.int8);
+        if (GATED) keep8(raw2, eight(raw2), rec + a.padded + c, rec + a.codes + a.scales + (u >> 2), on, a.int8);
+      }
+    } else if (on) {
+      const F8 z = decode8(w, s, a.int8);
+      T *out = row(a.out, a.pitch_out);
+      Out8<T> dz, du, f;
+      if (OP == kLoad) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dz.set(j, z.p[j]);
+        put8<T, VEC>(out, c, limit, dz);
+        return;
+      }
+      F8 up;
+      if (GATED) up = decode8(w2, s2, a.int8);
+      const F8 d = eight(raw);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t v = act2<T, ACT>(z.p[j], &slope);
+        if (GATED) {
+          du.set(j, pair_mul(v, d.p[j]));
+          dz.set(j, pair_mul(pair_mul(slope, up.p[j]), d.p[j]));
+          f.set(j, pair_mul(v, up.p[j]));
         } else {
-          Raw8<T> raw;
-          fetch8<T, VEC>(raw, (const T *)a.in + b * a.ld_in, c, limit);
-          const F8 z = decode8(w, s, a.int8), d = eight(raw);
-          F8 slope, f = act8<T, ACT>(z, &slope);
-          T *out = (T *)a.out + b * a.ld_out;
-          if (GATED) {
-            const F8 up = decode8(w2, s2, a.int8);
-            put8<T, VEC>(out + a.cols, c, limit, f * d);
-            slope = slope * up, f = f * up;
-          }
-          put8<T, VEC>(out, c, limit, slope * d);
-          if (a.again) put8<T, VEC>((T *)a.again + b * a.ld_again, c, limit, f);
+          dz.set(j, pair_mul(slope, d.p[j]));
+          f.set(j, v);
         }
       }
+      put8<T, VEC>(out, c, limit, dz);
+      if (GATED) put8<T, VEC>(out + a.cols, c, limit, du);
+      if (a.again) put8<T, VEC>(row(a.again, a.pitch_again), c, limit, f);
+    }
+  }
+};
+
+// Two pieces of a thread are on their way at a time; one of a gated matrix, whose registers are better spent on threads (two: 312 us against
+// 300 at 16384 x 6144).  Small CTAs, as many as there are tiles: 512 threads 331 us, 256 302, 128 295, forty registers or more alike.
+template <typename T, int OP, int ACT, bool GATED, bool VEC>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 12 : 9) ckpt_kernel(const CkptArgs args) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (int64_t row0 = (int64_t)blockIdx.x * args.tile_rows; row0 < args.M; row0 += (int64_t)gridDim.x * args.tile_rows) {
+    const int n = (int)min((int64_t)args.tile_rows, args.M - row0) * args.units;   // (a multiple of four: a block is whole)
+    CkptArgs a = args;
+    a.in += row0 * args.pitch_in, a.out += row0 * args.pitch_out, a.again = args.again ? args.again + row0 * args.pitch_again : nullptr;
+    a.ckpt = args.ckpt ? args.ckpt + row0 * args.row_bytes : nullptr;
+    for (int i = threadIdx.x; i - (int)threadIdx.x < n; i += (GATED ? 1 : 2) * kThreads) {
+      Piece<T, OP, GATED, VEC> p, q;
+      p.ask(a, i, n);
+      if (!GATED) q.ask(a, i + kThreads, n);
+      p.template finish<ACT>(a);
+      if (!GATED) q.template finish<ACT>(a);
     }
   }
 }
 
 template <typename T, int OP, int ACT, bool GATED>
 cudaError_t launch_ckpt(const alg_ckpt_s &h, CkptArgs a, bool vec, cudaStream_t st) {
-  a.row_bytes = h.row_bytes;
-  a.cols = h.cols, a.padded = h.padded, a.parts = h.parts;
+  a.row_bytes = (uint32_t)h.row_bytes;
+  a.cols = h.cols, a.padded = h.padded, a.codes = h.parts * h.padded, a.scales = h.padded / kBlock;
   a.units = h.padded / 8;
   a.inv_units = (uint32_t)((0x100000000ull + a.units - 1) / a.units);
   a.int8 = h.format == ALG_Q8_INT8;
@@ -287,7 +348,7 @@ cudaError_t launch_ckpt(const alg_ckpt_s &h, CkptArgs a, bool vec, cudaStream_t 
   a.tile_rows = a.units >= 4 * kThreads ? 1 : 4 * kThreads / a.units;
   const int64_t tiles = (a.M + a.tile_rows - 1) / a.tile_rows;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles < (int64_t)h.num_sms * 64 ? tiles : (int64_t)h.num_sms * 64));
+  cfg.gridDim = dim3((unsigned)tiles);   // (2^30 rows at most)
   cfg.blockDim = dim3(kThreads);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -361,10 +422,10 @@ alg_status_t alg_ckpt_store(alg_ckpt_t h, const void *X, int64_t ldx, alg_dtype_
   alg_status_t s = ckpt_common(h, M, x_dtype);
   if (s != ALG_OK || M == 0) return s;
   const size_t e = elem_size(x_dtype);
-  if (h->parts != 1 || !X || !ckpt || ldx < h->cols || !on_element(X, e) || ((uintptr_t)ckpt & 15u)) return ALG_ERR_INVALID_ARG;
+  if (h->parts != 1 || !X || !ckpt || ldx < h->cols || ldx >= kMaxLd || !on_element(X, e) || ((uintptr_t)ckpt & 15u)) return ALG_ERR_INVALID_ARG;
   if (meet(span(X, ldx, h->cols, e, M), records(*h, ckpt, M)) || !is_current(h->device)) return ALG_ERR_INVALID_ARG;
   CkptArgs a = {};
-  a.in = X, a.ld_in = ldx, a.ckpt = (uint8_t *)ckpt, a.M = M;
+  a.in = (const uint8_t *)X, a.pitch_in = (uint32_t)(ldx * e), a.ckpt = (uint8_t *)ckpt, a.M = M;
   const bool vec = vectors(*h, X, ldx, e);
   cudaStream_t st = (cudaStream_t)stream;
   return ckpt_done(x_dtype == ALG_BF16 ? launch_ckpt<__nv_bfloat16, kStore, ALG_ACT_NONE, false>(*h, a, vec, st)
@@ -375,10 +436,10 @@ alg_status_t alg_ckpt_load(alg_ckpt_t h, const void *ckpt, int64_t M, void *X, i
   alg_status_t s = ckpt_common(h, M, x_dtype);
   if (s != ALG_OK || M == 0) return s;
   const size_t e = elem_size(x_dtype);
-  if (h->parts != 1 || !X || !ckpt || ldx < h->cols || !on_element(X, e) || ((uintptr_t)ckpt & 15u)) return ALG_ERR_INVALID_ARG;
+  if (h->parts != 1 || !X || !ckpt || ldx < h->cols || ldx >= kMaxLd || !on_element(X, e) || ((uintptr_t)ckpt & 15u)) return ALG_ERR_INVALID_ARG;
   if (meet(span(X, ldx, h->cols, e, M), records(*h, ckpt, M)) || !is_current(h->device)) return ALG_ERR_INVALID_ARG;
   CkptArgs a = {};
-  a.out = X, a.ld_out = ldx, a.ckpt = (uint8_t *)ckpt, a.M = M;
+  a.out = (uint8_t *)X, a.pitch_out = (uint32_t)(ldx * e), a.ckpt = (uint8_t *)ckpt, a.M = M;
   const bool vec = vectors(*h, X, ldx, e);
   cudaStream_t st = (cudaStream_t)stream;
   return ckpt_done(x_dtype == ALG_BF16 ? launch_ckpt<__nv_bfloat16, kLoad, ALG_ACT_NONE, false>(*h, a, vec, st)
@@ -391,11 +452,11 @@ alg_status_t alg_ckpt_act_forward(alg_ckpt_t h, const void *Z, int64_t ldz, int6
   if (s != ALG_OK || M == 0) return s;
   const size_t e = elem_size(dtype);
   const int64_t wide = (int64_t)h->parts * h->cols;
-  if (!Z || !A || ldz < wide || lda < h->cols || !on_element(Z, e) || !on_element(A, e) || ((uintptr_t)ckpt & 15u)) return ALG_ERR_INVALID_ARG;
+  if (!Z || !A || ldz < wide || lda < h->cols || ldz >= kMaxLd || lda >= kMaxLd || !on_element(Z, e) || !on_element(A, e) || ((uintptr_t)ckpt & 15u)) return ALG_ERR_INVALID_ARG;
   const RowSpan z = span(Z, ldz, wide, e, M), out = span(A, lda, h->cols, e, M), rec = records(*h, ckpt, M);
   if ((meet(out, z) && !same_rows(out, z)) || meet(rec, z) || meet(rec, out) || !is_current(h->device)) return ALG_ERR_INVALID_ARG;
   CkptArgs a = {};
-  a.in = Z, a.ld_in = ldz, a.out = A, a.ld_out = lda, a.ckpt = (uint8_t *)ckpt, a.M = M;
+  a.in = (const uint8_t *)Z, a.pitch_in = (uint32_t)(ldz * e), a.out = (uint8_t *)A, a.pitch_out = (uint32_t)(lda * e), a.ckpt = (uint8_t *)ckpt, a.M = M;
   const bool vec = vectors(*h, Z, ldz, e) && vectors(*h, A, lda, e);
   cudaStream_t st = (cudaStream_t)stream;
   return ckpt_done(dtype == ALG_BF16 ? launch_act<__nv_bfloat16, kForward>(*h, a, vec, st) : launch_act<float, kForward>(*h, a, vec, st));
@@ -407,7 +468,7 @@ alg_status_t alg_ckpt_act_backward(alg_ckpt_t h, const void *ckpt, const void *d
   if (s != ALG_OK || M == 0) return s;
   const size_t e = elem_size(dtype);
   const int64_t wide = (int64_t)h->parts * h->cols;
-  if (!ckpt || !dA || !dZ || ldda < h->cols || lddz < wide || (A && lda < h->cols) || !on_element(dA, e) || !on_element(dZ, e) || !on_element(A, e) ||
+  if (!ckpt || !dA || !dZ || ldda < h->cols || lddz < wide || (A && lda < h->cols) || ldda >= kMaxLd || lddz >= kMaxLd || lda >= kMaxLd || !on_element(dA, e) || !on_element(dZ, e) || !on_element(A, e) ||
       ((uintptr_t)ckpt & 15u))
     return ALG_ERR_INVALID_ARG;
   const RowSpan g = span(dA, ldda, h->cols, e, M), out = span(dZ, lddz, wide, e, M), again = span(A, lda, h->cols, e, M), rec = records(*h, ckpt, M);
@@ -415,7 +476,8 @@ alg_status_t alg_ckpt_act_backward(alg_ckpt_t h, const void *ckpt, const void *d
       !is_current(h->device))
     return ALG_ERR_INVALID_ARG;
   CkptArgs a = {};
-  a.in = dA, a.ld_in = ldda, a.out = dZ, a.ld_out = lddz, a.again = A, a.ld_again = lda, a.ckpt = (uint8_t *)ckpt, a.M = M;
+  a.in = (const uint8_t *)dA, a.pitch_in = (uint32_t)(ldda * e), a.out = (uint8_t *)dZ, a.pitch_out = (uint32_t)(lddz * e), a.again = (uint8_t *)A,
+  a.pitch_again = (uint32_t)(lda * e), a.ckpt = (uint8_t *)ckpt, a.M = M;
   const bool vec = vectors(*h, dA, ldda, e) && vectors(*h, dZ, lddz, e) && vectors(*h, A, lda, e);
   cudaStream_t st = (cudaStream_t)stream;
   return ckpt_done(dtype == ALG_BF16 ? launch_act<__nv_bfloat16, kBackward>(*h, a, vec, st) : launch_act<float, kBackward>(*h, a, vec, st));

@@ -140,7 +140,6 @@ cudaError_t launch_norm(const alg_norm_s &h, NormArgs &a, bool vec, bool *full, 
   return h.dtype == ALG_BF16 ? launch_any<BACK, float, __nv_bfloat16>(a, w, vec, *grid, smem, st) : launch_any<BACK, float, float>(a, w, vec, *grid, smem, st);
 }
 
-constexpr int64_t kMaxLd = 1 << 30;   // (the kernels count the bytes between rows in 32 bits)
 void put_operand(NormArgs &a, int k, const void *p, int64_t ld, size_t e) { a.op[k] = (const uint8_t *)p, a.pitch[k] = (uint32_t)(ld * e); }
 // One matrix operand: its span, whether it is well formed, whether its rows lie on 16 bytes.
 struct Operand {

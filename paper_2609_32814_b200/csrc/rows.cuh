@@ -137,6 +137,7 @@ __device__ __forceinline__ float sigmoid(float x) {
   return r;
 }
 
+constexpr int64_t kMaxLd = 1 << 30;   // (the kernels count the bytes between rows in 32 bits)
 inline size_t elem_size(alg_dtype_t t) { return t == ALG_BF16 ? 2 : 4; }
 inline bool on_16(const void *p, int64_t ld, size_t elem) { return ((uintptr_t)p & 15u) == 0 && ((size_t)ld * elem) % 16 == 0; }
 inline bool on_element(const void *p, size_t elem) { return (uintptr_t)p % elem == 0; }
