@@ -143,8 +143,8 @@ def prepare(case, seed):
         if own:
             from paper_2609_32814_b200 import binding
             s["norm"] = binding.BlockNorm(d, kind=c["kind"], join=True, post=c["post"], pre=c["pre"],
-                                          gate=None if c["gate"] == "none" else c["gate"], gate_act="sigmoid" if c["sigmoid"] else None,
-                                          eps=EPS, dtype=c["dtype"], stream_dtype=c["stream"])
+                                          gate=None if c["gate"] == "none" else c["gate"],
+                                          gate_act="sigmoid" if c["sigmoid"] and c["gate"] != "none" else None, eps=EPS, dtype=c["dtype"], stream_dtype=c["stream"])
         return s
     if c["use"] in ("act", "ckpt"):
         m, n = c["m"], c["d"] if c["use"] == "ckpt" else c["f"] * (2 if c["gated"] else 1)
