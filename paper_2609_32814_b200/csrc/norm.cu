@@ -62,13 +62,13 @@ __global__ void __launch_bounds__(32 * kSlices) norm_sums_kernel(const SumsArgs 
 }
 
 // Threads of a row, rows a CTA works on at once, rows on their way; the grid.
-int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool full, bool back, size_t *smem) {
+int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool vec, bool full, bool back, size_t *smem) {
   a.T = (a.D + 256 * v - 1) / (256 * v) * 32;
   a.stage_bytes = 0;
   for (int k = 0; k < kOps; ++k) {
     a.at[k] = a.stage_bytes;
     a.bytes[k] = (uint32_t)(a.D * elem_size(k < kN ? h.stream_dtype : h.dtype));
-    if (a.op[k]) a.stage_bytes += (int)((a.bytes[k] + 15) / 16 * 16);
+    if (a.op[k]) a.stage_bytes += (int)((a.bytes[k] + (vec ? 15 : 30)) / 16 * 16);   // (a row off 16 bytes brings up to 15 on either side)
   }
   const size_t stage = a.stage_bytes;
   const int kept = ((a.flags & ALG_NORM_JOIN ? 1 : 0) + (a.flags & ALG_NORM_PRE ? 1 : 0)) * (full ? 2 : 1);
@@ -121,7 +121,7 @@ cudaError_t launch_norm(const alg_norm_s &h, NormArgs &a, bool vec, bool *full, 
   bool form = vec && h.dtype == ALG_BF16 && *full == (a.layer != 0);
   if (BACK) form = form && a.op[kT] && (!join || a.out) && (!gated || a.dg) && v == (a.layer ? 1 : 2);
   if (form) {
-    *grid = shape_rows(h, a, v, *full, BACK, &smem);
+    *grid = shape_rows(h, a, v, vec, *full, BACK, &smem);
     form = a.vectors > 0;
   }
   if (form) {
@@ -133,7 +133,7 @@ cudaError_t launch_norm(const alg_norm_s &h, NormArgs &a, bool vec, bool *full, 
   }
   *full = true;
   const int w = eights(BACK, true, a.D);
-  *grid = shape_rows(h, a, w, true, BACK, &smem);
+  *grid = shape_rows(h, a, w, vec, true, BACK, &smem);
   if (h.stream_dtype == ALG_BF16)
     return h.dtype == ALG_BF16 ? launch_any<BACK, __nv_bfloat16, __nv_bfloat16>(a, w, vec, *grid, smem, st)
                                : launch_any<BACK, __nv_bfloat16, float>(a, w, vec, *grid, smem, st);

@@ -234,44 +234,38 @@ __device__ __forceinline__ F8 vector8(const NormArgs &a, const Vectors &vec, int
 
 // A row of the operands on its way into shared memory.  The warps of a group share the asking: a copy takes its thread about 150
 // cycles, and a warp that asked for all five would have the others wait at the next barrier.  (What has landed before it is expected
-// only makes the barrier's count negative for a while.)
+// only makes the barrier's count negative for a while.)  A row off 16 bytes comes with the rest of the 16-byte words that hold its ends, and lies
+// as far into its place in the stage as it does into the first of them.
+template <bool OFF>
 __device__ __forceinline__ void issue_row(const NormArgs &a, uint32_t stage, uint32_t bar, uint32_t row, int t) {
   if (t & 31) return;
+  auto from = [&](int k) { return a.op[k] + (uint64_t)row * a.pitch[k]; };
+  auto bytes = [&](int k) { return OFF ? (((uint32_t)(uintptr_t)from(k) & 15u) + a.bytes[k] + 15u) & ~15u : a.bytes[k]; };
   if (t == 0) {
     uint32_t total = 0;
 #pragma unroll
-    for (int k = 0; k < kOps; ++k) total += a.op[k] ? a.bytes[k] : 0u;
+    for (int k = 0; k < kOps; ++k) total += a.op[k] ? bytes(k) : 0u;
     tc::mbar_expect_tx(bar, total);
   }
   for (int k = t >> 5; k < kOps; k += a.T >> 5)
     if (a.op[k])
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(stage + a.at[k]),
-                   "l"(a.op[k] + (uint64_t)row * a.pitch[k]), "r"(a.bytes[k]), "r"(bar)
+                   "l"((uintptr_t)from(k) & ~(uintptr_t)15), "r"(bytes(k)), "r"(bar)
                    : "memory");
 }
-// Unaligned rows: the group copies them itself.
-template <typename XT, typename BT>
-__device__ __forceinline__ void copy_row(const NormArgs &a, uint8_t *stage, uint32_t row, int t) {
-#pragma unroll
-  for (int k = 0; k < kOps; ++k) {
-    if (!a.op[k]) continue;
-    const uint8_t *p = a.op[k] + (uint64_t)row * a.pitch[k];
-    for (int c = t; c < a.D; c += a.T) {
-      if (k < kN) ((XT *)(stage + a.at[k]))[c] = ((const XT *)p)[c];
-      else ((BT *)(stage + a.at[k]))[c] = ((const BT *)p)[c];
-    }
-  }
+template <typename T, int MAP>
+__device__ __forceinline__ const T *staged(const NormArgs &a, const uint8_t *stage, int k, uint32_t row) {
+  return (const T *)(stage + a.at[k] + (MAP == kScalar ? ((uint32_t)(uintptr_t)a.op[k] + row * a.pitch[k]) & 15u : 0u));
 }
 
 // The loop over a group's rows: body(row, stage, release); release() once the row's operands are read and a barrier of the group has
 // followed.
 template <int MAP, int V, typename XT, typename BT, typename Body>
 __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vectors *vec, bool full, Body body) {
-  constexpr bool copies = MAP == kScalar;
   const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
   uint8_t *const rows = smem + kRowsAt + a.vectors + g * a.stages * a.stage_bytes;
   const uint32_t bar = tc::smem_u32(smem) + g * a.stages * 8, rows_at = tc::smem_u32(rows);
-  if (!copies && t == 0) {
+  if (t == 0) {
     for (int s = 0; s < a.stages; ++s) tc::mbar_init(bar + 8 * s, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -279,20 +273,15 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t first = blockIdx.x * a.G + g, step = gridDim.x * a.G;
-  if (!copies)
-    for (int s = 0; s < a.stages; ++s)
-      if (first + s * step < a.M) issue_row(a, rows_at + s * a.stage_bytes, bar + 8 * s, first + s * step, t);
+  for (int s = 0; s < a.stages; ++s)
+    if (first + s * step < a.M) issue_row<MAP == kScalar>(a, rows_at + s * a.stage_bytes, bar + 8 * s, first + s * step, t);
   *vec = fold_vectors<MAP, V>(a, smem, full);
   __syncthreads();
   int s = 0;
   uint32_t parity = 0;
   bool failed = false;   // after a wait that ran out nothing is right, but every thread still goes the same way to the end
   for (uint32_t row = first; row < a.M; row += step) {
-    if (copies) {
-      group_barrier(g, a.T);   // (the row before it is read)
-      copy_row<XT, BT>(a, rows, row, t);
-      group_barrier(g, a.T);
-    } else if (!tc::mbar_try_wait(bar + 8 * s, parity) && !failed) {
+    if (!tc::mbar_try_wait(bar + 8 * s, parity) && !failed) {
       const long long t0 = clock64();
       while (!tc::mbar_try_wait(bar + 8 * s, parity))
         if (clock64() - t0 > a.wait_limit) {
@@ -302,9 +291,9 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
         }
     }
     body(row, (const uint8_t *)rows + s * a.stage_bytes, [&] {
-      if (!copies && row + a.stages * step < a.M) issue_row(a, rows_at + s * a.stage_bytes, bar + 8 * s, row + a.stages * step, t);
+      if (row + a.stages * step < a.M) issue_row<MAP == kScalar>(a, rows_at + s * a.stage_bytes, bar + 8 * s, row + a.stages * step, t);
     });
-    if (!copies && ++s == a.stages) s = 0, parity ^= 1;
+    if (++s == a.stages) s = 0, parity ^= 1;
   }
 }
 
@@ -357,12 +346,12 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArg
       return rsqrtf(s[0] * inv_d + a.eps);
     };
 #pragma unroll
-    for (int v = 0; v < V; ++v) y[v] = cols.load((const XT *)(st + a.at[kX]), v);
+    for (int v = 0; v < V; ++v) y[v] = cols.load(staged<XT, MAP>(a, st, kX, row), v);
     if (join) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        f[v] = cols.load((const BT *)(st + a.at[kF]), v);
-        if (gate_el) q[v] = cols.load((const BT *)(st + a.at[kG]), v);
+        f[v] = cols.load(staged<BT, MAP>(a, st, kF, row), v);
+        if (gate_el) q[v] = cols.load(staged<BT, MAP>(a, st, kG, row), v);
       }
       const float rf = post ? stat(f) : 1.f, g1 = gate_row && sig ? sigmoid(gate) : gate;
 #pragma unroll
@@ -427,21 +416,21 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
   each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
     // a row of eight columns a thread stays in registers, a wider one is read from its stage as needed
     F8 hx, hn, hf, hh;   // (hh: dN * pre_weight)
-    auto x_of = [&](int v) { return V == 1 ? hx : cols.load((const XT *)(st + a.at[kX]), v); };
-    auto n_of = [&](int v) { return V == 1 ? hn : cols.load((const BT *)(st + a.at[kN]), v); };
+    auto x_of = [&](int v) { return V == 1 ? hx : cols.load(staged<XT, MAP>(a, st, kX, row), v); };
+    auto n_of = [&](int v) { return V == 1 ? hn : cols.load(staged<BT, MAP>(a, st, kN, row), v); };
     auto h_of = [&](int v) { return V == 1 ? hh : n_of(v) * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v); };
-    auto f_of = [&](int v) { return V == 1 ? hf : cols.load((const BT *)(st + a.at[kF]), v); };
+    auto f_of = [&](int v) { return V == 1 ? hf : cols.load(staged<BT, MAP>(a, st, kF, row), v); };
     F8 d[V], q[V];   // dY, then the gradient of R; the gate
     bool held = V == 1;
     const float gate_1 = gate_row ? next_gate((const BT *)a.gate, row, a, gate_ahead) : 1.f;
     if (V == 1) {
-      if (pre) hx = cols.load((const XT *)(st + a.at[kX]), 0), hn = cols.load((const BT *)(st + a.at[kN]), 0), hh = hn * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, 0);
-      if (join) hf = cols.load((const BT *)(st + a.at[kF]), 0);
+      if (pre) hx = cols.load(staged<XT, MAP>(a, st, kX, row), 0), hn = cols.load(staged<BT, MAP>(a, st, kN, row), 0), hh = hn * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, 0);
+      if (join) hf = cols.load(staged<BT, MAP>(a, st, kF, row), 0);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      d[v] = has_dy ? cols.load((const XT *)(st + a.at[kT]), v) : all8(0.f);
-      if (V == 1 && gate_el) q[v] = cols.load((const BT *)(st + a.at[kG]), v);
+      d[v] = has_dy ? cols.load(staged<XT, MAP>(a, st, kT, row), v) : all8(0.f);
+      if (V == 1 && gate_el) q[v] = cols.load(staged<BT, MAP>(a, st, kG, row), v);
     }
     // statistics of Y and F, and the means of h = dN * pre_weight and of h times the normed Y
     float mx = 0.f, mf = 0.f, mh = 0.f;
@@ -503,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
       F8 dg = d[v] * gr;   // the gradient behind the gate
       F8 slope;
       if (gate_el) {
-        F8 z = V == 1 ? q[v] : cols.load((const BT *)(st + a.at[kG]), v);
+        F8 z = V == 1 ? q[v] : cols.load(staged<BT, MAP>(a, st, kG, row), v);
         if (sig) {
           float p[8];
           to8(z, p);
