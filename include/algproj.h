@@ -413,7 +413,8 @@ alg_status_t alg_moe_last_status(alg_moe_t h, void *stream, alg_status_t *status
  *                  dgate = T .* scale .* (V .* post_weight + post_bias) (times the sigmoid's slope; summed over a row for GATE_ROW),
  *              and the column sums d_post_weight, d_post_bias, d_scale, d_pre_weight, d_pre_bias (D fp32 values each, overwritten; NULL:
  *              not wanted; the biases' need no biases in the forward pass).  dF needs JOIN, dgate a gate flag, d_post_* POST, d_pre_*
- *              PRE, d_scale JOIN; dF and dgate may be NULL.  Sums run in a fixed order: bitwise repeatable.
+ *              PRE, d_scale JOIN; dF and dgate may be NULL.  Sums run in a fixed order: bitwise repeatable
+ *              (which order depends on the types, the sizes and how the rows lie in their 16-byte words).
  * 1 <= D <= ALG_NORM_MAX_D.  Leading dimensions (below 2^30) and addresses may be anything an element may have; D a multiple of 8 with all
  * rows on 16 bytes (vectors too) runs several times faster.  Row b of an output may lie exactly on row b of an operand (Y on R, dR on
  * dY, ...: same address, leading dimension and row length in bytes); any other overlap is ALG_ERR_INVALID_ARG.  M = 0: forward

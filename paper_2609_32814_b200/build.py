@@ -14,7 +14,11 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libalgproj.so")
-SOURCES = ["api.cu", "bucket.cu", "proj_simt.cu", "proj_tc.cu", "proj_tc2.cu", "proj_split.cu", "proj_big.cu", "decode.cu", "ffn_decode.cu", "row_decode.cu", "static_ws.cu", "ckpt.cu", "norm.cu", "norm_forward_bf16.cu", "norm_forward_f32.cu", "norm_backward_bf16.cu", "norm_backward_f32.cu", "moe.cu"]
+# (the ones that take long first)
+SOURCES = ["norm_backward_any.cu", "norm_backward_any_wide.cu", "norm_backward_layer_bf16.cu", "norm_backward_layer_f32.cu", "norm_backward_rms_bf16.cu",
+           "norm_backward_rms_f32.cu", "norm_forward_bf16.cu", "norm_forward_f32.cu", "ffn_decode.cu", "proj_tc.cu", "proj_big.cu", "row_decode.cu",
+           "norm_forward_any.cu", "api.cu", "bucket.cu", "proj_simt.cu", "proj_tc2.cu", "proj_split.cu", "decode.cu", "static_ws.cu", "ckpt.cu", "norm.cu",
+           "moe.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
@@ -47,7 +51,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             raise RuntimeError(f"nvcc failed on {src}")
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(sources)) as ex:
+    with ThreadPoolExecutor(max_workers=os.cpu_count() or 8) as ex:
         objs = list(ex.map(compile_one, sources))
     tmp = LIB + f".tmp{os.getpid()}"
     subprocess.check_call([_nvcc(), "-shared", "-cudart", "static", "-o", tmp, *objs])

@@ -1,4 +1,4 @@
-// C-ABI entry points of a block's border, the kernels that find out their form at run time, and the second launch of the column sums.
+// C-ABI entry points of a block's border, and the second launch of the column sums.
 #include <cmath>
 #include <new>
 
@@ -62,13 +62,14 @@ __global__ void __launch_bounds__(32 * kSlices) norm_sums_kernel(const SumsArgs 
 }
 
 // Threads of a row, rows a CTA works on at once, rows on their way; the grid.
-int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool vec, bool full, bool back, size_t *smem) {
-  a.T = (a.D + 256 * v - 1) / (256 * v) * 32;
+int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool full, bool back, size_t *smem) {
+  const int most_off = a.period > 1 || a.off ? 7 : 0;   // a shifted row's places
+  a.T = (a.D + most_off + 256 * v - 1) / (256 * v) * 32;
   a.stage_bytes = 0;
   for (int k = 0; k < kOps; ++k) {
     a.at[k] = a.stage_bytes;
     a.bytes[k] = (uint32_t)(a.D * elem_size(k < kN ? h.stream_dtype : h.dtype));
-    if (a.op[k]) a.stage_bytes += (int)((a.bytes[k] + (vec ? 15 : 30)) / 16 * 16);   // (a row off 16 bytes brings up to 15 on either side)
+    if (a.op[k]) a.stage_bytes += (int)((a.bytes[k] + 30) / 16 * 16);   // (a row off 16 bytes brings up to 15 on either side)
   }
   const size_t stage = a.stage_bytes;
   const int kept = ((a.flags & ALG_NORM_JOIN ? 1 : 0) + (a.flags & ALG_NORM_PRE ? 1 : 0)) * (full ? 2 : 1);
@@ -77,81 +78,92 @@ int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool vec, bool full, boo
   const size_t budget = (size_t)kBudget - a.vectors;
   int groups = kThreads / a.T;
   if (groups > kMaxGroups) groups = kMaxGroups;
-  const int64_t per_sm = (a.M + h.num_sms - 1) / h.num_sms;
+  const int64_t rows_of = (a.M + a.period - 1) / a.period, sms = h.num_sms / a.period;   // rows of a shift, CTAs for them
+  const int64_t per_sm = (rows_of + sms - 1) / sms;
   if (groups > per_sm) groups = (int)per_sm;
   while (groups > 1 && 2 * groups * stage > budget) --groups;   // (a row ahead of each)
   a.G = groups;
   int stages = (int)(budget / (groups * stage));
   if (stages > kMaxStages) stages = kMaxStages;
-  const int64_t rows = (a.M + (int64_t)groups * h.num_sms - 1) / ((int64_t)groups * h.num_sms);
+  const int64_t rows = (rows_of + (int64_t)groups * sms - 1) / ((int64_t)groups * sms);
   if (stages > rows) stages = (int)rows;
   a.stages = stages;
   size_t bytes = (size_t)groups * stages * stage;
   if (back && bytes < (size_t)groups * a.D * 4) bytes = (size_t)groups * a.D * 4;   // the groups' sums meet there
   *smem = kRowsAt + a.vectors + bytes;
-  const int64_t ctas = (a.M + groups - 1) / groups;
-  return (int)(ctas < h.num_sms ? ctas : h.num_sms);
+  const int64_t ctas = (rows_of + groups - 1) / groups;
+  return (int)(ctas < sms ? ctas : sms) * a.period;
 }
 
+// Values that are accessed at once.
+int granule(const alg_norm_s &h) { return h.stream_dtype == ALG_BF16 && h.dtype == ALG_BF16 ? 8 : 4; }
 // Columns a thread has, in eights.  The sums of LayerNorm's backward pass (four a column) leave registers for eight columns; all else takes
 // sixteen, which halves what a row costs each thread besides its columns (32768 x 4096 forward 274 against 265 us, gradients of 8003 x 1024 47 against 40).
 int eights(bool back, bool full, int D) { return back && full && D <= kNarrow ? 1 : 2; }
 
-template <bool BACK, typename XT, typename BT, int V>
-cudaError_t launch_any(NormArgs &a, bool vec, int grid, size_t smem, cudaStream_t st) {
-  constexpr int kMap = sizeof(XT) == 4 || sizeof(BT) == 4 ? kFours : kEight;
-  return vec ? launch_rows<BACK, XT, BT, kMap, V, true, kAny>(a, grid, smem, st) : launch_rows<BACK, XT, BT, kScalar, V, true, kAny>(a, grid, smem, st);
-}
-template <bool BACK, typename XT, typename BT>
-cudaError_t launch_any(NormArgs &a, int v, bool vec, int grid, size_t smem, cudaStream_t st) {
-  if constexpr (BACK)
-    if (v == 1) return launch_any<BACK, XT, BT, 1>(a, vec, grid, smem, st);
-  return launch_any<BACK, XT, BT, 2>(a, vec, grid, smem, st);
-}
-
-// *full: LayerNorm or biases (set here; the caller asks for gradients of biases).  Kernels with their form as a constant serve bf16 F, gate and N
-// on 16 bytes, with dY and all gradients in the backward pass, LayerNorm (with or without biases) or RMS norm without biases, whose
-// folded vectors fit.
+// *full: LayerNorm or biases (set here; the caller asks for gradients of biases).  Kernels with their form as a constant serve bf16 F, gate and N, with dY and all gradients in the backward pass, LayerNorm (with or without biases) or RMS norm without biases, whose
+// folded vectors fit.  alike: the matrices lie off their granules alike; on16: they and the vectors lie on 16 bytes.
 template <bool BACK>
-cudaError_t launch_norm(const alg_norm_s &h, NormArgs &a, bool vec, bool *full, int *grid, cudaStream_t st) {
+cudaError_t launch_norm(const alg_norm_s &h, NormArgs &a, bool alike, bool on16, bool *full, int *grid, cudaStream_t st) {
   size_t smem = 0;
   *full = *full || a.layer || a.post_b || a.pre_b;
   const int v = eights(BACK, *full, a.D);
   const bool gated = a.flags & (ALG_NORM_GATE_ROW | ALG_NORM_GATE_ELEMENT), join = a.flags & ALG_NORM_JOIN;
-  bool form = vec && h.dtype == ALG_BF16 && *full == (a.layer != 0);
+  bool form = alike && (a.flags & (ALG_NORM_PRE | ALG_NORM_POST)) && h.dtype == ALG_BF16 && *full == (a.layer != 0);
   if (BACK) form = form && a.op[kT] && (!join || a.out) && (!gated || a.dg) && v == (a.layer ? 1 : 2);
   if (form) {
-    *grid = shape_rows(h, a, v, vec, *full, BACK, &smem);
+    *grid = shape_rows(h, a, v, *full, BACK, &smem);
     form = a.vectors > 0;
   }
   if (form) {
-    const int gate = !gated ? kGateNone : a.flags & ALG_NORM_GATE_ROW ? kGateRow : a.flags & ALG_NORM_GATE_SIGMOID ? kGateSigmoid : kGateElement;
+    const int gate = !gated ? kGateNone : a.flags & ALG_NORM_GATE_ROW ? kGateRow : kGateElement;
     const int f = (a.flags & ALG_NORM_PRE ? kFormPre : 0) | (a.flags & ALG_NORM_POST ? kFormPost : 0) | (join ? kFormJoin : 0);
-    auto *launch = BACK ? (h.stream_dtype == ALG_BF16 ? launch_norm_backward_bf16 : launch_norm_backward_f32)
-                        : (h.stream_dtype == ALG_BF16 ? launch_norm_forward_bf16 : launch_norm_forward_f32);
-    return launch(a, f + kFormGate * gate, a.layer, *grid, smem, st);
+    const bool bf16 = h.stream_dtype == ALG_BF16;
+    if constexpr (BACK) {
+      auto *launch = a.layer ? (bf16 ? launch_norm_backward_layer_bf16 : launch_norm_backward_layer_f32)
+                             : (bf16 ? launch_norm_backward_rms_bf16 : launch_norm_backward_rms_f32);
+      return launch(a, f + kFormGate * gate, on16, *grid, smem, st);
+    } else {
+      return (bf16 ? launch_norm_forward_bf16 : launch_norm_forward_f32)(a, f + kFormGate * gate, a.layer, on16, *grid, smem, st);
+    }
   }
   *full = true;
   const int w = eights(BACK, true, a.D);
-  *grid = shape_rows(h, a, w, vec, true, BACK, &smem);
-  if (h.stream_dtype == ALG_BF16)
-    return h.dtype == ALG_BF16 ? launch_any<BACK, __nv_bfloat16, __nv_bfloat16>(a, w, vec, *grid, smem, st)
-                               : launch_any<BACK, __nv_bfloat16, float>(a, w, vec, *grid, smem, st);
-  return h.dtype == ALG_BF16 ? launch_any<BACK, float, __nv_bfloat16>(a, w, vec, *grid, smem, st) : launch_any<BACK, float, float>(a, w, vec, *grid, smem, st);
+  *grid = shape_rows(h, a, w, true, BACK, &smem);
+  const bool exact = on16 && a.D % granule(h) == 0;
+  const int types = (h.stream_dtype == ALG_F32 ? 2 : 0) + (h.dtype == ALG_F32 ? 1 : 0);
+  auto *launch = !BACK ? launch_norm_forward_any : w == 1 ? launch_norm_backward_any : launch_norm_backward_any_wide;
+  return launch(a, types, alike, exact, *grid, smem, st);
 }
 
 void put_operand(NormArgs &a, int k, const void *p, int64_t ld, size_t e) { a.op[k] = (const uint8_t *)p, a.pitch[k] = (uint32_t)(ld * e); }
-// One matrix operand: its span, whether it is well formed, whether its rows lie on 16 bytes.
+// One matrix operand: its span, and whether it is well formed.
 struct Operand {
   RowSpan s;
-  bool ok, vec;
+  bool ok;
 };
 Operand operand(const void *p, int64_t ld, int64_t cols, size_t e, int64_t M) {
-  if (!p) return {span(nullptr, 0, 0, 1, 0), true, true};
-  return {span(p, ld, cols, e, M), ld >= cols && ld < kMaxLd && on_element(p, e), on_16(p, ld, e)};
+  if (!p) return {span(nullptr, 0, 0, 1, 0), true};
+  return {span(p, ld, cols, e, M), ld >= cols && ld < kMaxLd && on_element(p, e)};
 }
 bool vector_ok(const float *p) { return on_element(p, 4); }
-bool vector_16(const float *p) { return ((uintptr_t)p & 15u) == 0; }
+// Whether all matrices lie off their granules alike (`unit` values: eight where all are bf16, else four); how.
+struct Granules {
+  int unit;
+  bool any = false, alike = true, on16 = true;   // on16: all rows on 16 bytes
+  int off = 0, ld_off = 0;
+  void add(const void *p, int64_t ld, size_t e, int64_t M) {
+    if (!p) return;
+    const int o = (int)((uintptr_t)p / e % unit), l = M > 1 ? (int)(ld % unit) : 0;
+    on16 = on16 && on_16(p, M > 1 ? ld : 0, e);
+    if (any && (o != off || l != ld_off)) alike = false;
+    any = true, off = o, ld_off = l;
+  }
+  void tell(NormArgs &a) const {
+    a.off = alike ? off : 0, a.ld_off = alike ? ld_off : 0, a.period = 1;
+    while (a.period * a.ld_off % unit) a.period *= 2;
+  }
+};
 size_t sums_bytes(const alg_norm_s &h) { return (size_t)h.num_sms * kSums * h.D * sizeof(float); }
 
 }  // namespace
@@ -213,21 +225,18 @@ alg_status_t alg_norm_forward(alg_norm_t h, const void *R, int64_t ldr, const vo
   const int D = h->D;
   const Operand in[3] = {operand(R, ldr, D, ex, M), operand(F, ldf, D, eb, M), row ? operand(gate, 1, 1, eb, M) : operand(gate, ldg, D, eb, M)};
   const Operand to[2] = {operand(Y, ldy, D, ex, M), operand(N, ldn, D, eb, M)};
-  bool vec = D % 8 == 0;
   for (const Operand &o : to) {
     if (!o.ok) return ALG_ERR_INVALID_ARG;
-    vec = vec && o.vec;
     for (const Operand &i : in)
       if (meet(o.s, i.s) && !same_rows(o.s, i.s)) return ALG_ERR_INVALID_ARG;
   }
-  for (int k = 0; k < 3; ++k) {
-    if (!in[k].ok) return ALG_ERR_INVALID_ARG;
-    vec = vec && (in[k].vec || (k == 2 && row));
-  }
+  for (const Operand &i : in)
+    if (!i.ok) return ALG_ERR_INVALID_ARG;
   if (meet(to[0].s, to[1].s)) return ALG_ERR_INVALID_ARG;
+  bool on16 = true;   // the vectors
   for (const float *v : {post_weight, post_bias, scale, pre_weight, pre_bias}) {
     if (!vector_ok(v)) return ALG_ERR_INVALID_ARG;
-    vec = vec && vector_16(v);
+    on16 = on16 && ((uintptr_t)v & 15u) == 0;
     for (const Operand &o : to)
       if (v && meet(o.s, span(v, D, D, 4, 1))) return ALG_ERR_INVALID_ARG;
   }
@@ -239,9 +248,12 @@ alg_status_t alg_norm_forward(alg_norm_t h, const void *R, int64_t ldr, const vo
   a.post_w = post_weight, a.post_b = post_bias, a.scale = scale, a.pre_w = pre_weight, a.pre_b = pre_bias;
   a.y = (uint8_t *)Y, a.pitch_y = (uint32_t)(ldy * ex), a.out = (uint8_t *)N, a.pitch_out = (uint32_t)(ldn * eb);
   a.status = h->d_status, a.wait_limit = kDefaultWaitLimit;
+  Granules gr = {granule(*h)};
+  gr.add(R, ldr, ex, M), gr.add(F, ldf, eb, M), gr.add(el ? gate : nullptr, ldg, eb, M), gr.add(Y, ldy, ex, M), gr.add(N, ldn, eb, M);
+  gr.tell(a);
   int grid = 0;
   bool full = false;
-  return launch_norm<false>(*h, a, vec, &full, &grid, (cudaStream_t)stream) == cudaSuccess ? ALG_OK : ALG_ERR_CUDA;
+  return launch_norm<false>(*h, a, gr.alike, on16 && gr.on16, &full, &grid, (cudaStream_t)stream) == cudaSuccess ? ALG_OK : ALG_ERR_CUDA;
 }
 
 alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const void *dY, int64_t lddy, const void *dN, int64_t lddn, const void *F,
@@ -259,13 +271,14 @@ alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const v
   const int D = h->D;
   float *const vectors_out[5] = {d_post_weight, d_post_bias, d_scale, d_pre_weight, d_pre_bias};
   const float *const vectors_in[4] = {post_weight, post_bias, scale, pre_weight};
-  bool vec = D % 8 == 0;
+  bool on16 = true;   // the vectors
   for (const float *v : vectors_out)
     if (!vector_ok(v)) return ALG_ERR_INVALID_ARG;
   for (const float *v : vectors_in) {
     if (!vector_ok(v)) return ALG_ERR_INVALID_ARG;
-    vec = vec && vector_16(v);
+    on16 = on16 && ((uintptr_t)v & 15u) == 0;
   }
+  Granules gr = {granule(*h)};
   if (sums && (!workspace || ((uintptr_t)workspace & 255u))) return ALG_ERR_INVALID_ARG;
   if (sums && workspace_bytes < sums_bytes(*h)) return ALG_ERR_WORKSPACE_TOO_SMALL;
   NormArgs a = {};
@@ -279,13 +292,11 @@ alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const v
     const RowSpan ws = sums ? span(workspace, 0, (int64_t)sums_bytes(*h), 1, 1) : span(nullptr, 0, 0, 1, 0);
     for (int k = 0; k < 5; ++k) {
       if (!in[k].ok || meet(ws, in[k].s)) return ALG_ERR_INVALID_ARG;
-      vec = vec && (in[k].vec || (k == 4 && row));
       for (const float *v : vectors_out)
         if (v && meet(in[k].s, span(v, D, D, 4, 1))) return ALG_ERR_INVALID_ARG;
     }
     for (int k = 0; k < 3; ++k) {
       if (!to[k].ok || meet(ws, to[k].s)) return ALG_ERR_INVALID_ARG;
-      vec = vec && (to[k].vec || (k == 2 && row));
       for (const Operand &i : in)
         if (meet(to[k].s, i.s) && !same_rows(to[k].s, i.s)) return ALG_ERR_INVALID_ARG;
       for (int l = 0; l < k; ++l)
@@ -299,6 +310,9 @@ alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const v
     put_operand(a, kT, dY, lddy, ex), put_operand(a, kN, dN, lddn, eb), put_operand(a, kF, F, ldf, eb);
     put_operand(a, kG, el ? gate : nullptr, ldg, eb);
     a.gate = row ? gate : nullptr;
+    gr.add(pre ? Y : nullptr, ldy, ex, M), gr.add(dY, lddy, ex, M), gr.add(dN, lddn, eb, M), gr.add(F, ldf, eb, M), gr.add(el ? gate : nullptr, ldg, eb, M);
+    gr.add(dR, lddr, ex, M), gr.add(dF, lddf, eb, M), gr.add(el ? dgate : nullptr, lddg, eb, M);
+    gr.tell(a);
     a.y = (uint8_t *)dR, a.pitch_y = (uint32_t)(lddr * ex), a.out = (uint8_t *)dF, a.pitch_out = (uint32_t)(lddf * eb);
     a.dg = (uint8_t *)dgate, a.pitch_dg = (uint32_t)(lddg * eb);
   }
@@ -310,7 +324,7 @@ alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const v
   a.status = h->d_status, a.wait_limit = kDefaultWaitLimit;
   int grid = 0;
   bool full = d_post_bias || d_pre_bias;
-  if (M > 0 && launch_norm<true>(*h, a, vec, &full, &grid, st) != cudaSuccess) return ALG_ERR_CUDA;
+  if (M > 0 && launch_norm<true>(*h, a, gr.alike, on16 && gr.on16, &full, &grid, st) != cudaSuccess) return ALG_ERR_CUDA;
   if (!sums) return ALG_OK;
   SumsArgs b = {grid, D, h->flags, full, alpha, a.part, post_weight, post_bias, scale, d_post_weight, d_post_bias, d_scale, d_pre_weight, d_pre_bias};
   void *params[] = {&b};

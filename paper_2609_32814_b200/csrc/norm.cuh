@@ -20,11 +20,18 @@
 namespace algproj {
 
 struct NormArgs;
-// One translation unit for each direction and type of the residual stream (F, gate and N bf16): the kernels with their form as a constant.
-cudaError_t launch_norm_forward_bf16(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
-cudaError_t launch_norm_forward_f32(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
-cudaError_t launch_norm_backward_bf16(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
-cudaError_t launch_norm_backward_f32(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st);
+// A translation unit each for a direction and type of the residual stream (F, gate and N bf16), and in the backward pass for a norm: the kernels with their form as a constant.
+// types: 2 for an fp32 stream, + 1 for fp32 F, gate and N; alike: see NormArgs::off; exact:
+// rows of whole granules on 16 bytes.
+cudaError_t launch_norm_forward_any(NormArgs &a, int types, bool alike, bool exact, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_any(NormArgs &a, int types, bool alike, bool exact, int grid, size_t smem, cudaStream_t st);   // rows of eight columns a thread
+cudaError_t launch_norm_backward_any_wide(NormArgs &a, int types, bool alike, bool exact, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_forward_bf16(NormArgs &a, int form, bool layer, bool on16, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_forward_f32(NormArgs &a, int form, bool layer, bool on16, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_rms_bf16(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_layer_bf16(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_rms_f32(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_layer_f32(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
 
 
 constexpr int kMaxStages = 4;
@@ -44,6 +51,7 @@ struct NormArgs {
   const uint8_t *op[kOps];      // rows of the operands, nullptr for none
   uint32_t pitch[kOps], bytes[kOps];   // bytes between rows, of a row
   int at[kOps], stage_bytes;    // where a row lies in a stage
+  int period, off, ld_off;      // rows whose first value lies off a granule of 4 or 8: by (off + row * ld_off) mod granule, the same every `period` rows
   const void *gate;             // of each row
   const float *post_w, *post_b, *scale, *pre_w, *pre_b;
   uint8_t *y, *out;             // forward: Y, N; backward: dR, dF
@@ -58,7 +66,7 @@ struct NormArgs {
 // The form of a call: what it does, as a constant of a kernel (kAny: found out at run time, with every branch that costs: gradients of
 // 16384 x 4096 rows 467 us against 320).
 enum { kFormPre = 1, kFormPost = 2, kFormJoin = 4, kFormGate = 8, kAny = -1 };   // + kFormGate * gate
-enum { kGateNone, kGateRow, kGateElement, kGateSigmoid };   // a row's gate asks for its sigmoid at run time
+enum { kGateNone, kGateRow, kGateElement };   // (whether through a sigmoid is asked at run time)
 
 namespace {
 
@@ -119,71 +127,99 @@ __device__ __forceinline__ void group_sum(float (&v)[K], float4 *red, int &turn,
 // A thread's pieces of eight columns.  Rows on 16 bytes: eight consecutive ones, or, where operands are fp32, four and four that lie
 // T * 4 columns apart (eight fp32 values in a row would have every second thread's 16 bytes meet in the same banks).  Else every T-th
 // column, whose scalar accesses coalesce.
-// kWhole: every thread's pieces are inside the row, nothing is asked.
-enum { kScalar, kEight, kFours, kWhole = 4 };
+// Rows need not begin on a granule (eight bf16 values, four fp32): where all operands lie off it alike, a CTA takes rows that lie off it by the same
+// `shift`, and column c is at c + shift of the granules, so that accesses are whole ones all the same; threads at a row's ends mask theirs.
+// kExact: no shift, and every granule is inside the row or outside; all rows and vectors lie on 16 bytes.  kWhole: and inside, all of them
+// (nothing is asked, which the backward pass has no registers for: gradients of 16384 x 4096 rows 265 us against 311).
+enum { kScalar, kEight, kFours, kExact = 4, kWhole = 8 + kExact };
 template <int HOW>
 struct Cols {
   static constexpr int MAP = HOW & 3;
-  int t, T, D;
+  int t, T, shift, end;   // end: D + shift
   __device__ __forceinline__ int at(int v, int j) const {
     return MAP == kEight ? (v * T + t) * 8 + j : MAP == kFours ? ((2 * v + (j >> 2)) * T + t) * 4 + (j & 3) : t + (v * 8 + j) * T;
   }
-  __device__ __forceinline__ bool on(int v, int j) const { return HOW & kWhole || at(v, MAP == kEight ? 0 : MAP == kFours ? j & 4 : j) < D; }
+  __device__ __forceinline__ bool on(int v, int j) const {
+    if ((HOW & kWhole) == kWhole) return true;
+    if (HOW & kExact) return at(v, MAP == kEight ? 0 : j & 4) < end;
+    return at(v, j) >= shift && at(v, j) < end;
+  }
+  // granule `from` (its first value's place) of `n`: some of it inside the row; all of it
+  __device__ __forceinline__ bool some(int from) const { return (HOW & kWhole) == kWhole || from < end; }
+  __device__ __forceinline__ bool all(int from, int n) const { return HOW & kExact ? some(from) : from >= shift && from + n <= end; }
   template <typename T_>
-  __device__ __forceinline__ F8 load(const T_ *row, int v) const {   // zero past the row's end
+  __device__ __forceinline__ F8 load(const T_ *row, int v) const {   // zero outside the row
     float f[8];
-    if (MAP == kEight) {
-      Raw8<T_> r;
-      if (on(v, 0)) r.load(row + at(v, 0));
-      else r.zero();
-      r.get(f);
-    } else if (MAP == kFours) {
-      Raw8<T_> r;
-      r.zero();
-      if (on(v, 0)) r.load4(0, row + at(v, 0));
-      if (on(v, 4)) r.load4(1, row + at(v, 4));
-      r.get(f);
-    } else {
+    if (MAP == kScalar) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = on(v, j) ? to_f32(row[at(v, j)]) : 0.f;
+      return from8(f);
     }
-    return from8(f);
+    Raw8<T_> r;
+    if (MAP == kEight) {
+      if (some(at(v, 0))) r.load(row + at(v, 0));
+      else r.zero();
+    } else {
+      if ((HOW & kWhole) != kWhole) r.zero();
+      if (some(at(v, 0))) r.load4(0, row + at(v, 0));
+      if (some(at(v, 4))) r.load4(1, row + at(v, 4));
+    }
+    r.get(f);
+    return HOW & kExact ? from8(f) : inside(from8(f), v);
   }
   template <typename T_>
   __device__ __forceinline__ void store(T_ *row, int v, const F8 &a) const {
     float f[8];
     to8(a, f);
-    if (MAP == kEight) {
-      if (on(v, 0)) store8(row + at(v, 0), f);
-    } else if (MAP == kFours) {
-      if (on(v, 0)) store4(row + at(v, 0), f[0], f[1], f[2], f[3]);
-      if (on(v, 4)) store4(row + at(v, 4), f[4], f[5], f[6], f[7]);
+    if (HOW & kExact) {
+      if (MAP == kEight) {
+        if (some(at(v, 0))) store8(row + at(v, 0), f);
+      } else {
+        if (some(at(v, 0))) store4(row + at(v, 0), f[0], f[1], f[2], f[3]);
+        if (some(at(v, 4))) store4(row + at(v, 4), f[4], f[5], f[6], f[7]);
+      }
+    } else if (MAP == kEight && all(at(v, 0), 8)) {
+      store8(row + at(v, 0), f);
+    } else if (MAP == kFours && all(at(v, 0), 4) && all(at(v, 4), 4)) {
+      store4(row + at(v, 0), f[0], f[1], f[2], f[3]);
+      store4(row + at(v, 4), f[4], f[5], f[6], f[7]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (on(v, j)) from_f32(f[j], row + at(v, j));
     }
   }
-  // `a` inside the row, zero past its end
+  // `a` inside the row, zero outside
   __device__ __forceinline__ F8 inside(const F8 &a, int v) const {
-    if (HOW & kWhole) return a;
-    if (MAP == kEight) return on(v, 0) ? a : all8(0.f);
+    if ((HOW & kWhole) == kWhole) return a;
+    if (HOW & kExact && MAP == kEight) return some(at(v, 0)) ? a : all8(0.f);
+    if (MAP == kEight && all(at(v, 0), 8)) return a;
+    if (MAP == kFours && all(at(v, 0), 4) && all(at(v, 4), 4)) return a;
     float f[8];
     to8(a, f);
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = on(v, j) ? f[j] : 0.f;
     return from8(f);
   }
-  // Where the folded vectors keep a column: for consecutive eights in two planes of fours, again for the banks.
+  // Where the folded vectors keep a place: for consecutive eights in two planes of fours, again for the banks.
   __device__ __forceinline__ static int kept(int c, int pieces) { return MAP == kEight ? ((c >> 2 & 1) * pieces + (c >> 3)) * 4 + (c & 3) : c; }
   __device__ __forceinline__ F8 load_kept(const float *vec, int v, int pieces) const {
-    if (MAP != kEight) return load(vec, v);
     float f[8];
-    const float4 a = *(const float4 *)(vec + (v * T + t) * 4), b = *(const float4 *)(vec + (pieces + v * T + t) * 4);
+    if (MAP == kScalar) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = vec[at(v, j)];
+      return from8(f);
+    }
+    const float4 a = *(const float4 *)(vec + (MAP == kEight ? (v * T + t) * 4 : at(v, 0))), b = *(const float4 *)(vec + (MAP == kEight ? (pieces + v * T + t) * 4 : at(v, 4)));
     f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
     return from8(f);
   }
 };
+template <int HOW>
+__device__ __forceinline__ int shift_of(const NormArgs &a) {
+  if (HOW & kExact || HOW == kScalar) return 0;
+  return (a.off + (int)(blockIdx.x % a.period) * a.ld_off) & ((HOW & 3) == kEight ? 7 : 3);
+}
 
 // The vectors of a call, folded: in shared memory where that leaves room for the rows, else read from where they lie.
 enum { kVecW, kVecB, kVecPreW, kVecPreB };   // alpha * scale * post_weight, alpha * scale * post_bias, pre_weight, pre_bias
@@ -211,12 +247,15 @@ __device__ __forceinline__ Vectors fold_vectors(const NormArgs &a, uint8_t *smem
   for (int k = 0; k < 4; ++k) {
     const bool used = (k < 2 ? a.flags & ALG_NORM_JOIN : a.flags & ALG_NORM_PRE) && (full || !(k & 1));
     if (!used || !a.vectors) continue;
-    if (Cols<MAP>::MAP == kScalar) {
-      for (int c = threadIdx.x; c < a.T * V * 8; c += blockDim.x) to[c] = c < a.D ? Vectors::value(a, k, c) : 0.f;
-    } else {   // (D is a multiple of eight, and the vectors lie on 16 bytes)
+    const int shift = shift_of<MAP>(a);
+    if (MAP & kExact) {
 #pragma unroll 4
       for (int c = threadIdx.x * 4; c < a.T * V * 8; c += blockDim.x * 4)
         *(float4 *)(to + Cols<MAP>::kept(c, a.T * V)) = c < a.D ? Vectors::value4(a, k, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+#pragma unroll 4
+      for (int c = threadIdx.x; c < a.T * V * 8; c += blockDim.x)
+        to[Cols<MAP>::kept(c, a.T * V)] = c >= shift && c < a.D + shift ? Vectors::value(a, k, c - shift) : 0.f;
     }
     vec.at[k] = to;
     to += a.T * V * 8;
@@ -228,7 +267,7 @@ __device__ __forceinline__ F8 vector8(const NormArgs &a, const Vectors &vec, int
   if (V == 1 || FORM != kAny || a.vectors) return cols.load_kept(vec.at[which], v, a.T * V);
   float f[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = cols.on(v, j) ? Vectors::value(a, which, cols.at(v, j)) : 0.f;
+  for (int j = 0; j < 8; ++j) f[j] = cols.on(v, j) ? Vectors::value(a, which, cols.at(v, j) - cols.shift) : 0.f;
   return from8(f);
 }
 
@@ -254,9 +293,14 @@ __device__ __forceinline__ void issue_row(const NormArgs &a, uint32_t stage, uin
                    : "memory");
 }
 template <typename T, int MAP>
-__device__ __forceinline__ const T *staged(const NormArgs &a, const uint8_t *stage, int k, uint32_t row) {
-  return (const T *)(stage + a.at[k] + (MAP == kScalar ? ((uint32_t)(uintptr_t)a.op[k] + row * a.pitch[k]) & 15u : 0u));
+__device__ __forceinline__ const T *staged(const NormArgs &a, const uint8_t *stage, int k, uint32_t row, int shift) {
+  if (MAP & kExact) return (const T *)(stage + a.at[k]);
+  return (const T *)(stage + a.at[k] + (int)(((uint32_t)(uintptr_t)a.op[k] + row * a.pitch[k]) & 15u) - shift * (int)sizeof(T));
 }
+
+// A group's rows: those of its CTA's shift (the grid is a multiple of the period).
+__device__ __forceinline__ uint32_t row_step(const NormArgs &a) { return gridDim.x * a.G; }
+__device__ __forceinline__ uint32_t first_row(const NormArgs &a, int g) { return blockIdx.x % a.period + a.period * (blockIdx.x / a.period * a.G + g); }
 
 // The loop over a group's rows: body(row, stage, release); release() once the row's operands are read and a barrier of the group has
 // followed.
@@ -272,9 +316,9 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
   group_barrier(g, a.T);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint32_t first = blockIdx.x * a.G + g, step = gridDim.x * a.G;
+  const uint32_t first = first_row(a, g), step = row_step(a);
   for (int s = 0; s < a.stages; ++s)
-    if (first + s * step < a.M) issue_row<MAP == kScalar>(a, rows_at + s * a.stage_bytes, bar + 8 * s, first + s * step, t);
+    if (first + s * step < a.M) issue_row<!(MAP & kExact)>(a, rows_at + s * a.stage_bytes, bar + 8 * s, first + s * step, t);
   *vec = fold_vectors<MAP, V>(a, smem, full);
   __syncthreads();
   int s = 0;
@@ -291,7 +335,7 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
         }
     }
     body(row, (const uint8_t *)rows + s * a.stage_bytes, [&] {
-      if (row + a.stages * step < a.M) issue_row<MAP == kScalar>(a, rows_at + s * a.stage_bytes, bar + 8 * s, row + a.stages * step, t);
+      if (row + a.stages * step < a.M) issue_row<!(MAP & kExact)>(a, rows_at + s * a.stage_bytes, bar + 8 * s, row + a.stages * step, t);
     });
     if (++s == a.stages) s = 0, parity ^= 1;
   }
@@ -300,7 +344,7 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
 // The gate of a row, asked for one row ahead.
 template <typename BT>
 __device__ __forceinline__ float next_gate(const BT *gate, uint32_t row, const NormArgs &a, float &ahead) {
-  const uint32_t step = gridDim.x * a.G;
+  const uint32_t step = row_step(a);
   const float now = row < step ? to_f32(gate[row]) : ahead;   // (a group's first row is below the step)
   if (row + step < a.M) ahead = to_f32(gate[row + step]);
   return now;
@@ -312,14 +356,15 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArg
   extern __shared__ __align__(128) uint8_t smem[];
   float4 *red = (float4 *)(smem + kBarBytes);
   const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
-  const Cols<MAP> cols = {t, a.T, a.D};
+  const int shift = shift_of<MAP>(a);
+  const Cols<MAP> cols = {t, a.T, shift, a.D + shift};
   const float inv_d = 1.f / (float)a.D;
   constexpr bool any = FORM == kAny;
   constexpr int gate_of = any ? 0 : FORM / kFormGate;
   const bool pre = any ? a.flags & ALG_NORM_PRE : FORM & kFormPre, join = any ? a.flags & ALG_NORM_JOIN : FORM & kFormJoin;
   const bool post = any ? a.flags & ALG_NORM_POST : FORM & kFormPost, layer = any ? FULL && a.layer : FULL;
-  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of >= kGateElement;
-  const bool sig = any || gate_of == kGateRow ? a.flags & ALG_NORM_GATE_SIGMOID : gate_of == kGateSigmoid;
+  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of == kGateElement;
+  const bool sig = (any || gate_of) && a.flags & ALG_NORM_GATE_SIGMOID;
   int turn = 0;
   Vectors vec;
   float gate_ahead = 0.f;
@@ -346,12 +391,12 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArg
       return rsqrtf(s[0] * inv_d + a.eps);
     };
 #pragma unroll
-    for (int v = 0; v < V; ++v) y[v] = cols.load(staged<XT, MAP>(a, st, kX, row), v);
+    for (int v = 0; v < V; ++v) y[v] = cols.load(staged<XT, MAP>(a, st, kX, row, shift), v);
     if (join) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        f[v] = cols.load(staged<BT, MAP>(a, st, kF, row), v);
-        if (gate_el) q[v] = cols.load(staged<BT, MAP>(a, st, kG, row), v);
+        f[v] = cols.load(staged<BT, MAP>(a, st, kF, row, shift), v);
+        if (gate_el) q[v] = cols.load(staged<BT, MAP>(a, st, kG, row, shift), v);
       }
       const float rf = post ? stat(f) : 1.f, g1 = gate_row && sig ? sigmoid(gate) : gate;
 #pragma unroll
@@ -371,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArg
         } else {
           y[v] = fma8(n, g1, y[v]);
         }
-        cols.store((XT *)(a.y + (uint64_t)row * a.pitch_y), v, y[v]);
+        cols.store((XT *)(a.y + (uint64_t)row * a.pitch_y) - shift, v, y[v]);
       }
     }
     if (pre) {
@@ -380,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArg
       for (int v = 0; v < V; ++v) {
         F8 n = y[v] * ry * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v);
         if (FULL) n = n + vector8<MAP, V, FORM>(a, vec, kVecPreB, cols, v);
-        cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out), v, n);
+        cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out) - shift, v, n);
       }
     }
     if (held) {
@@ -395,14 +440,15 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
   extern __shared__ __align__(128) uint8_t smem[];
   float4 *red = (float4 *)(smem + kBarBytes);
   const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
-  const Cols<MAP> cols = {t, a.T, a.D};
+  const int shift = shift_of<MAP>(a);
+  const Cols<MAP> cols = {t, a.T, shift, a.D + shift};
   const float inv_d = 1.f / (float)a.D;
   constexpr bool any = FORM == kAny;
   constexpr int gate_of = any ? 0 : FORM / kFormGate;
   const bool pre = any ? a.flags & ALG_NORM_PRE : FORM & kFormPre, join = any ? a.flags & ALG_NORM_JOIN : FORM & kFormJoin;
   const bool post = any ? a.flags & ALG_NORM_POST : FORM & kFormPost, layer = any ? FULL && a.layer : FULL;
-  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of >= kGateElement;
-  const bool sig = any || gate_of == kGateRow ? a.flags & ALG_NORM_GATE_SIGMOID : gate_of == kGateSigmoid;
+  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of == kGateElement;
+  const bool sig = (any || gate_of) && a.flags & ALG_NORM_GATE_SIGMOID;
   // (a form that is a constant comes with dY and with every gradient wanted)
   const bool has_dy = any ? a.op[kT] != nullptr : true, to_f = any ? a.out != nullptr : true, to_gate = any ? a.dg != nullptr : true;
   F8 sum[kSums][V];
@@ -416,21 +462,21 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
   each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
     // a row of eight columns a thread stays in registers, a wider one is read from its stage as needed
     F8 hx, hn, hf, hh;   // (hh: dN * pre_weight)
-    auto x_of = [&](int v) { return V == 1 ? hx : cols.load(staged<XT, MAP>(a, st, kX, row), v); };
-    auto n_of = [&](int v) { return V == 1 ? hn : cols.load(staged<BT, MAP>(a, st, kN, row), v); };
+    auto x_of = [&](int v) { return V == 1 ? hx : cols.load(staged<XT, MAP>(a, st, kX, row, shift), v); };
+    auto n_of = [&](int v) { return V == 1 ? hn : cols.load(staged<BT, MAP>(a, st, kN, row, shift), v); };
     auto h_of = [&](int v) { return V == 1 ? hh : n_of(v) * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, v); };
-    auto f_of = [&](int v) { return V == 1 ? hf : cols.load(staged<BT, MAP>(a, st, kF, row), v); };
+    auto f_of = [&](int v) { return V == 1 ? hf : cols.load(staged<BT, MAP>(a, st, kF, row, shift), v); };
     F8 d[V], q[V];   // dY, then the gradient of R; the gate
     bool held = V == 1;
     const float gate_1 = gate_row ? next_gate((const BT *)a.gate, row, a, gate_ahead) : 1.f;
     if (V == 1) {
-      if (pre) hx = cols.load(staged<XT, MAP>(a, st, kX, row), 0), hn = cols.load(staged<BT, MAP>(a, st, kN, row), 0), hh = hn * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, 0);
-      if (join) hf = cols.load(staged<BT, MAP>(a, st, kF, row), 0);
+      if (pre) hx = cols.load(staged<XT, MAP>(a, st, kX, row, shift), 0), hn = cols.load(staged<BT, MAP>(a, st, kN, row, shift), 0), hh = hn * vector8<MAP, V, FORM>(a, vec, kVecPreW, cols, 0);
+      if (join) hf = cols.load(staged<BT, MAP>(a, st, kF, row, shift), 0);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      d[v] = has_dy ? cols.load(staged<XT, MAP>(a, st, kT, row), v) : all8(0.f);
-      if (V == 1 && gate_el) q[v] = cols.load(staged<BT, MAP>(a, st, kG, row), v);
+      d[v] = has_dy ? cols.load(staged<XT, MAP>(a, st, kT, row, shift), v) : all8(0.f);
+      if (V == 1 && gate_el) q[v] = cols.load(staged<BT, MAP>(a, st, kG, row, shift), v);
     }
     // statistics of Y and F, and the means of h = dN * pre_weight and of h times the normed Y
     float mx = 0.f, mf = 0.f, mh = 0.f;
@@ -486,13 +532,13 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
         d[v] = fma8(fma8(x, -mhv, h), rx, d[v]);
         if (layer) d[v] = cols.inside(d[v], v);
       }
-      cols.store((XT *)(a.y + (uint64_t)row * a.pitch_y), v, d[v]);
+      cols.store((XT *)(a.y + (uint64_t)row * a.pitch_y) - shift, v, d[v]);
       if (!join) continue;
       const F8 f = fc_of(v) * rf, w = vector8<MAP, V, FORM>(a, vec, kVecW, cols, v);
       F8 dg = d[v] * gr;   // the gradient behind the gate
       F8 slope;
       if (gate_el) {
-        F8 z = V == 1 ? q[v] : cols.load(staged<BT, MAP>(a, st, kG, row), v);
+        F8 z = V == 1 ? q[v] : cols.load(staged<BT, MAP>(a, st, kG, row, shift), v);
         if (sig) {
           float p[8];
           to8(z, p);
@@ -512,7 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
         b = b * d[v];
         if (gate_el) {
           if (sig) b = b * slope;
-          cols.store((BT *)(a.dg + (uint64_t)row * a.pitch_dg), v, b);
+          cols.store((BT *)(a.dg + (uint64_t)row * a.pitch_dg) - shift, v, b);
         } else {
           m[2] += sum8(b);
         }
@@ -521,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
         if (layer) m[0] += sum8(e[v]);
         m[1] += dot8(e[v], f);
       } else if (to_f) {
-        cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out), v, e[v]);
+        cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out) - shift, v, e[v]);
       }
     }
     if (join && ((post && to_f) || (gate_row && to_gate))) {
@@ -534,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
         for (int v = 0; v < V; ++v) {
           F8 o = fma8(fc_of(v) * rf, -mev, e[v]);
           if (layer) o = o + -me;
-          cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out), v, o * rf);
+          cols.store((BT *)(a.out + (uint64_t)row * a.pitch_out) - shift, v, o * rf);
         }
       }
     }
@@ -557,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
       to8(sum[k][v], f);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (cols.on(v, j)) acc[g * a.D + cols.at(v, j)] = f[j];
+        if (cols.on(v, j)) acc[g * a.D + cols.at(v, j) - shift] = f[j];
     }
     __syncthreads();
     for (int c = threadIdx.x; c < a.D; c += blockDim.x) {
@@ -598,31 +644,31 @@ cudaError_t launch_rows(NormArgs &a, int grid, size_t smem, cudaStream_t st) {
   return launch_norm_kernel(k, grid, a.T * a.G, smem, st, params);
 }
 
-// The kernel of a form: rows that fill the threads' pieces, or not.
+// The kernel of a form.
 template <bool BACK, typename XT, int V, bool LAYER, int FORM>
-cudaError_t launch_form(NormArgs &a, int grid, size_t smem, cudaStream_t st) {
+cudaError_t launch_form(NormArgs &a, bool on16, int grid, size_t smem, cudaStream_t st) {
   constexpr int kMap = sizeof(XT) == 4 ? kFours : kEight;
-  return a.D == a.T * V * 8 ? launch_rows<BACK, XT, __nv_bfloat16, kMap | kWhole, V, LAYER, FORM>(a, grid, smem, st)
-                            : launch_rows<BACK, XT, __nv_bfloat16, kMap, V, LAYER, FORM>(a, grid, smem, st);
+  // forward: rows of whole granules on 16 bytes; backward: such as fill the threads' pieces
+  if (on16 && (BACK ? a.D == a.T * V * 8 : a.D % (kMap == kEight ? 8 : 4) == 0))
+    return launch_rows<BACK, XT, __nv_bfloat16, kMap | (BACK ? kWhole : kExact), V, LAYER, FORM>(a, grid, smem, st);
+  return launch_rows<BACK, XT, __nv_bfloat16, kMap, V, LAYER, FORM>(a, grid, smem, st);
 }
 template <bool BACK, typename XT, int V, bool LAYER, int BASE>
-cudaError_t launch_gate(NormArgs &a, int gate, int grid, size_t smem, cudaStream_t st) {
+cudaError_t launch_gate(NormArgs &a, int gate, bool on16, int grid, size_t smem, cudaStream_t st) {
   switch (gate) {
-    case kGateNone: return launch_form<BACK, XT, V, LAYER, BASE>(a, grid, smem, st);
-    case kGateRow: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateRow>(a, grid, smem, st);
-    case kGateElement: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateElement>(a, grid, smem, st);
-    default: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateSigmoid>(a, grid, smem, st);
+    case kGateNone: return launch_form<BACK, XT, V, LAYER, BASE>(a, on16, grid, smem, st);
+    case kGateRow: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateRow>(a, on16, grid, smem, st);
+    default: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateElement>(a, on16, grid, smem, st);
   }
 }
 template <bool BACK, typename XT, int V, bool LAYER>
-cudaError_t launch_forms(NormArgs &a, int form, int grid, size_t smem, cudaStream_t st) {
+cudaError_t launch_forms(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st) {
   const int gate = form / kFormGate;
   switch (form % kFormGate) {
-    case kFormJoin | kFormPost | kFormPre: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPost | kFormPre>(a, gate, grid, smem, st);
-    case kFormJoin | kFormPost: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPost>(a, gate, grid, smem, st);
-    case kFormJoin | kFormPre: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPre>(a, gate, grid, smem, st);
-    case kFormJoin: return launch_gate<BACK, XT, V, LAYER, kFormJoin>(a, gate, grid, smem, st);
-    default: return launch_form<BACK, XT, V, LAYER, kFormPre>(a, grid, smem, st);
+    case kFormJoin | kFormPost | kFormPre: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPost | kFormPre>(a, gate, on16, grid, smem, st);
+    case kFormJoin | kFormPost: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPost>(a, gate, on16, grid, smem, st);
+    case kFormJoin | kFormPre: return launch_gate<BACK, XT, V, LAYER, kFormJoin | kFormPre>(a, gate, on16, grid, smem, st);
+    default: return launch_form<BACK, XT, V, LAYER, kFormPre>(a, on16, grid, smem, st);
   }
 }
 

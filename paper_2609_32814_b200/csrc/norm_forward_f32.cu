@@ -3,8 +3,8 @@
 
 namespace algproj {
 
-cudaError_t launch_norm_forward_f32(NormArgs &a, int form, bool layer, int grid, size_t smem, cudaStream_t st) {
-  return layer ? launch_forms<false, float, 2, true>(a, form, grid, smem, st) : launch_forms<false, float, 2, false>(a, form, grid, smem, st);
+cudaError_t launch_norm_forward_f32(NormArgs &a, int form, bool layer, bool on16, int grid, size_t smem, cudaStream_t st) {
+  return layer ? launch_forms<false, float, 2, true>(a, form, on16, grid, smem, st) : launch_forms<false, float, 2, false>(a, form, on16, grid, smem, st);
 }
 
 }  // namespace algproj

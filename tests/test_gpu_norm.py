@@ -166,7 +166,8 @@ FORMS = [  # kind, post, pre, gate, sigmoid, vectors
 
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("dtype,stream,m,d,pitch,at", [("bf16", "bf16", 1, 8, 0, 0), ("bf16", "f32", 37, 264, 272, 8), ("f32", "bf16", 5, 1000, 0, 0),
-                                                       ("bf16", "bf16", 9, 333, 335, 1), ("f32", "f32", 3, 1, 0, 0)])
+                                                       ("bf16", "bf16", 9, 333, 335, 1), ("f32", "f32", 3, 1, 0, 0),
+                                                       ("bf16", "f32", 37, 256, 260, 4), ("bf16", "bf16", 300, 513, 0, 0), ("bf16", "f32", 40, 770, 771, 3)])
 def test_border_and_its_gradients(form, dtype, stream, m, d, pitch, at):
     kind, post, pre, gate, sig, vectors = form
     b = Border(m, d, kind, post, pre, gate, sig, vectors, dtype, stream, pitch=pitch, at=at)
@@ -174,11 +175,12 @@ def test_border_and_its_gradients(form, dtype, stream, m, d, pitch, at):
     b.check_forward(y, n)
     got = b.h.backward(y, dY=b.dY, dN=b.dN if pre else None, **b.call(), out={"R": b.out["R"], "F": b.out["F"]})
     b.check_backward(y, got)
+    first = {k: v.clone() for k, v in got.items()}
+    again = b.h.backward(y, dY=b.dY, dN=b.dN if pre else None, **b.call(), out={"R": b.out["R"], "F": b.out["F"]})
+    for k in got:
+        assert torch.equal(first[k], again[k]), k                     # bitwise repeatable
     if pre:
         b.check_backward(y, b.h.backward(y, dN=b.dN, **b.call()), dy=False)
-    again = b.h.backward(y, dY=b.dY, dN=b.dN if pre else None, **b.call())
-    for k in got:
-        assert torch.equal(got[k], again[k]), k                       # bitwise repeatable
     for t in (b.R, b.F, b.out["Y"], b.out["R"]):                      # nothing between the rows was touched
         base = t._base if t._base is not None else t
         while base._base is not None:
@@ -191,13 +193,43 @@ def test_border_and_its_gradients(form, dtype, stream, m, d, pitch, at):
 
 @pytest.mark.parametrize("kind,dtype,stream,m,d", [("rms", "bf16", "bf16", 1999, 768), ("layer", "bf16", "f32", 700, 2048), ("rms", "f32", "f32", 300, 4096),
                                                    ("layer", "f32", "f32", 310, 8192), ("rms", "bf16", "bf16", 450, 7168), ("layer", "bf16", "bf16", 160, 4104),
-                                                   ("rms", "bf16", "f32", 155, 5003), ("layer", "bf16", "bf16", 2001, 96)])
+                                                   ("rms", "bf16", "f32", 155, 5003), ("layer", "bf16", "bf16", 2001, 96), ("rms", "bf16", "bf16", 1201, 1002), ("layer", "bf16", "f32", 903, 2047),
+                                                   ("rms", "bf16", "bf16", 333, 4097)])
 def test_many_rows(kind, dtype, stream, m, d):
     """More rows than a grid takes at once, every width of a thread's share, stages that wrap."""
     b = Border(m, d, kind, True, True, "element", True, True, dtype, stream)
     y, n = b.h.forward(b.R, **b.call())
     b.check_forward(y, n)
     b.check_backward(y, b.h.backward(y, dY=b.dY, dN=b.dN, **b.call()))
+
+
+@pytest.mark.parametrize("kind,back", [("rms", 0), ("layer", 0), ("rms", 1), ("layer", 1)])
+def test_operands_that_lie_off_sixteen_bytes_each_in_its_own_way(kind, back):
+    """Rows of R, F and the outputs begin at different places of a 16-byte word: single accesses, and the same results."""
+    b = Border(23, 520, kind, True, True, "element", False, True, "bf16", "bf16")
+    y, n = b.h.forward(b.R, **b.call())
+    want = b.h.backward(y, dY=b.dY, dN=b.dN, **b.call())
+
+    def moved(t, ld, at):
+        buf = torch.full((23 * ld + at + 8,), 3.0, dtype=t.dtype, device="cuda")
+        out = buf[at:at + 23 * ld].view(23, ld)[:, :520]
+        out.copy_(t)
+        return out, buf
+
+    r, f, g = moved(b.R, 521, 1)[0], moved(b.F, 523, 0)[0], moved(b.gate, 520, 5)[0]
+    out, buf = moved(b.R, 527, 3)
+    kw = dict(b.call(), F=f, gate=g)
+    if not back:
+        y2, n2 = b.h.forward(r, **kw, out=out)
+        # (sums run in another order: fp32 rounding, then one step of bf16 at most)
+        assert bool(((y2.float() - y.float()).abs() <= 2.0 ** -8 * y.float().abs() + 1e-6).all())
+        assert bool(((n2.float() - n.float()).abs() <= 2.0 ** -7 * n.float().abs() + 1e-5).all())
+        assert bool((buf[3:3 + 23 * 527].view(23, 527)[:, 520:] == 3.0).all() & (buf[:3] == 3.0).all() & (buf[-5:] == 3.0).all())
+        return
+    got = b.h.backward(moved(y, 525, 2)[0], dY=moved(b.dY, 522, 7)[0], dN=moved(b.dN, 520, 0)[0], **kw, out={"R": out})
+    for k in want:
+        size = float(want[k].float().abs().max())
+        assert bool(((got[k].float() - want[k].float()).abs() <= 2.0 ** -7 * want[k].float().abs() + 1e-5 * size).all()), k
 
 
 @pytest.mark.parametrize("kind", ["rms", "layer"])
