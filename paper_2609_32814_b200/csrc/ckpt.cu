@@ -178,38 +178,59 @@ struct Out8<__nv_bfloat16> {
     w[j] = *(const uint32_t *)&v;
   }
   __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]); }
-  __device__ __forceinline__ __nv_bfloat16 get(int j) const { return ((const __nv_bfloat16 *)w)[j]; }
+  __device__ __forceinline__ void stage(__nv_bfloat16 *p) const { store(p); }   // into shared memory
 };
 template <>
 struct Out8<float> {
   float f[8];
   __device__ __forceinline__ void set(int j, uint64_t p) { halves(p, f[2 * j], f[2 * j + 1]); }
   __device__ __forceinline__ void store(float *p) const { store8(p, f); }
-  __device__ __forceinline__ float get(int j) const { return f[j]; }
+  __device__ __forceinline__ void stage(float *p) const {
+    ((float4 *)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    ((float4 *)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  }
 };
 
-// Eight columns of a row from column c on, zero past `cols`.
-template <typename T, bool VEC>
+// Eight columns of a row from column c on, zero past `cols` (a multiple of 8), of rows on 16 bytes.
+template <typename T>
 __device__ __forceinline__ void fetch8(Raw8<T> &r, const T *row, int c, int cols) {
-  if (VEC) {
-    if (c < cols) r.load(row + c);   // (cols is a multiple of 8)
-    else r.zero();
-  } else {
-    r.zero();
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < cols) r.set(j, row[c + j]);
-  }
+  if (c < cols) r.load(row + c);
+  else r.zero();
 }
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void put8(T *row, int c, int cols, const Out8<T> &o) {
-  if (VEC) {
-    if (c < cols) o.store(row + c);
-  } else {
+  if (c < cols) o.store(row + c);
+}
+// The same of any rows, by whole warps: value by value, neighbouring threads on neighbouring columns, and turned round in the warp's part of
+// shared memory (eight values a thread straight from memory would be eight requests for the same sectors: 9000 x 4001 GELU 293 us).
+// r, c: the thread's row and column; c past the row for a thread without one.
+template <typename T>
+__device__ __forceinline__ void fetch_any(Raw8<T> &raw, T *turn, const uint8_t *base, uint32_t pitch, int first, uint32_t r, int c, int cols) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < cols) row[c + j] = o.get(j);
+  for (int j = 0; j < 8; ++j) {
+    const int from = j * 4 + (lane >> 3), col = __shfl_sync(~0u, c, from) + (lane & 7);
+    const uint32_t row = __shfl_sync(~0u, r, from);
+    T v = T(0.f);
+    if (col < cols) v = ((const T *)(base + (uint64_t)row * pitch))[first + col];
+    turn[j * 32 + lane] = v;
   }
+  __syncwarp();
+  raw.load(turn + lane * 8);
+  __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void put_any(const Out8<T> &o, T *turn, uint8_t *base, uint32_t pitch, int first, uint32_t r, int c, int cols) {
+  const int lane = threadIdx.x & 31;
+  o.stage(turn + lane * 8);
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int from = j * 4 + (lane >> 3), col = __shfl_sync(~0u, c, from) + (lane & 7);
+    const uint32_t row = __shfl_sync(~0u, r, from);
+    if (col < cols) ((T *)(base + (uint64_t)row * pitch))[first + col] = turn[j * 32 + lane];
+  }
+  __syncwarp();
 }
 
 // Whole warps call this: the maximum of a block is found among its four threads.
@@ -244,28 +265,35 @@ struct Piece {
 
   __device__ __forceinline__ T *row(uint8_t *p, uint32_t pitch) const { return (T *)(p + (uint64_t)r * pitch); }
   __device__ __forceinline__ uint8_t *record(const CkptArgs &a) const { return a.ckpt + (uint64_t)r * a.row_bytes; }
-  // piece i of n
-  __device__ __forceinline__ void ask(const CkptArgs &a, int i, int n) {
+  __device__ __forceinline__ int column() const { return on ? u * 8 : 1 << 30; }
+  __device__ __forceinline__ void fetch(Raw8<T> &v, const CkptArgs &a, int first, T *turn) const {
+    if (VEC) fetch8(v, row(const_cast<uint8_t *>(a.in), a.pitch_in) + first, column(), a.cols);
+    else fetch_any(v, turn, a.in, a.pitch_in, first, r, column(), a.cols);
+  }
+  __device__ __forceinline__ void put(const Out8<T> &v, const CkptArgs &a, uint8_t *to, uint32_t pitch, int first, T *turn) const {
+    if (VEC) put8(row(to, pitch) + first, column(), a.cols, v);
+    else put_any(v, turn, to, pitch, first, r, column(), a.cols);
+  }
+  // piece i of n; whole warps
+  __device__ __forceinline__ void ask(const CkptArgs &a, int i, int n, T *turn) {
     on = i < n;
     r = on ? __umulhi((uint32_t)i, a.inv_units) : 0u;
     u = on ? i - (int)r * a.units : 0;
-    const int c = u * 8, limit = on ? a.cols : 0;
     if (OP == kLoad || OP == kBackward) {
+      w = w2 = make_uint2(0u, 0u), s = s2 = 0;
       if (on) {
         const uint8_t *rec = record(a);
-        w = *(const uint2 *)(rec + c);
+        w = *(const uint2 *)(rec + u * 8);
         s = rec[a.codes + (u >> 2)];
-        if (GATED) w2 = *(const uint2 *)(rec + a.padded + c), s2 = rec[a.codes + a.scales + (u >> 2)];
+        if (GATED) w2 = *(const uint2 *)(rec + a.padded + u * 8), s2 = rec[a.codes + a.scales + (u >> 2)];
       }
     }
     if (OP == kLoad) return;
-    const T *in = row(const_cast<uint8_t *>(a.in), a.pitch_in);
-    fetch8<T, VEC>(raw, in, c, limit);
-    if (OP == kForward && GATED) fetch8<T, VEC>(raw2, in + a.cols, c, limit);
+    fetch(raw, a, 0, turn);
+    if (OP == kForward && GATED) fetch(raw2, a, a.cols, turn);
   }
   template <int ACT>
-  __device__ __forceinline__ void finish(const CkptArgs &a) {
-    const int c = u * 8, limit = on ? a.cols : 0;
+  __device__ __forceinline__ void finish(const CkptArgs &a, T *turn) {
     uint64_t slope;
     if (OP == kStore || OP == kForward) {
       if (OP == kForward) {
@@ -277,42 +305,41 @@ struct Piece {
           if (GATED) f = pair_mul(f, eight(raw2).p[j]);
           o.set(j, f);
         }
-        put8<T, VEC>(row(a.out, a.pitch_out), c, limit, o);
+        put(o, a, a.out, a.pitch_out, 0, turn);
       }
-      if (OP == kStore || a.ckpt) {   // (whole warps)
+      if (OP == kStore || a.ckpt) {
         uint8_t *rec = record(a);
-        keep8(raw, eight(raw), rec + c, rec + a.codes + (u >> 2), on, a.int8);
-        if (GATED) keep8(raw2, eight(raw2), rec + a.padded + c, rec + a.codes + a.scales + (u >> 2), on, a.int8);
+        keep8(raw, eight(raw), rec + u * 8, rec + a.codes + (u >> 2), on, a.int8);
+        if (GATED) keep8(raw2, eight(raw2), rec + a.padded + u * 8, rec + a.codes + a.scales + (u >> 2), on, a.int8);
       }
-    } else if (on) {
-      const F8 z = decode8(w, s, a.int8);
-      T *out = row(a.out, a.pitch_out);
-      Out8<T> dz, du, f;
-      if (OP == kLoad) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) dz.set(j, z.p[j]);
-        put8<T, VEC>(out, c, limit, dz);
-        return;
-      }
-      F8 up;
-      if (GATED) up = decode8(w2, s2, a.int8);
-      const F8 d = eight(raw);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint64_t v = act2<T, ACT>(z.p[j], &slope);
-        if (GATED) {
-          du.set(j, pair_mul(v, d.p[j]));
-          dz.set(j, pair_mul(pair_mul(slope, up.p[j]), d.p[j]));
-          f.set(j, pair_mul(v, up.p[j]));
-        } else {
-          dz.set(j, pair_mul(slope, d.p[j]));
-          f.set(j, v);
-        }
-      }
-      put8<T, VEC>(out, c, limit, dz);
-      if (GATED) put8<T, VEC>(out + a.cols, c, limit, du);
-      if (a.again) put8<T, VEC>(row(a.again, a.pitch_again), c, limit, f);
+      return;
     }
+    const F8 z = decode8(w, s, a.int8);
+    Out8<T> dz, du, f;
+    if (OP == kLoad) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dz.set(j, z.p[j]);
+      put(dz, a, a.out, a.pitch_out, 0, turn);
+      return;
+    }
+    F8 up;
+    if (GATED) up = decode8(w2, s2, a.int8);
+    const F8 d = eight(raw);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t v = act2<T, ACT>(z.p[j], &slope);
+      if (GATED) {
+        du.set(j, pair_mul(v, d.p[j]));
+        dz.set(j, pair_mul(pair_mul(slope, up.p[j]), d.p[j]));
+        f.set(j, pair_mul(v, up.p[j]));
+      } else {
+        dz.set(j, pair_mul(slope, d.p[j]));
+        f.set(j, v);
+      }
+    }
+    put(dz, a, a.out, a.pitch_out, 0, turn);
+    if (GATED) put(du, a, a.out, a.pitch_out, a.cols, turn);
+    if (a.again) put(f, a, a.again, a.pitch_again, 0, turn);
   }
 };
 
@@ -320,6 +347,8 @@ struct Piece {
 // 300 at 16384 x 6144).  Small CTAs, as many as there are tiles: 512 threads 331 us, 256 302, 128 295, forty registers or more alike.
 template <typename T, int OP, int ACT, bool GATED, bool VEC>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 12 : 9) ckpt_kernel(const CkptArgs args) {
+  __shared__ __align__(32) T turns[VEC ? 1 : kThreads / 32][VEC ? 1 : 256];
+  T *const turn = turns[VEC ? 0 : threadIdx.x >> 5];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   for (int64_t row0 = (int64_t)blockIdx.x * args.tile_rows; row0 < args.M; row0 += (int64_t)gridDim.x * args.tile_rows) {
@@ -329,10 +358,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 12 : 9) ckpt_kernel
     a.ckpt = args.ckpt ? args.ckpt + row0 * args.row_bytes : nullptr;
     for (int i = threadIdx.x; i - (int)threadIdx.x < n; i += (GATED ? 1 : 2) * kThreads) {
       Piece<T, OP, GATED, VEC> p, q;
-      p.ask(a, i, n);
-      if (!GATED) q.ask(a, i + kThreads, n);
-      p.template finish<ACT>(a);
-      if (!GATED) q.template finish<ACT>(a);
+      p.ask(a, i, n, turn);
+      if (!GATED) q.ask(a, i + kThreads, n, turn);
+      p.template finish<ACT>(a, turn);
+      if (!GATED) q.template finish<ACT>(a, turn);
     }
   }
 }
