@@ -466,6 +466,7 @@ class MoE(_Handle):
                                     {"softmax": ALG_MOE_SOFTMAX, "sigmoid": ALG_MOE_SIGMOID}[score], int(bool(renormalise)), float(route_scale),
                                     _DTYPES[router_dtype]), "alg_moe_create")
         self._device = torch.cuda.current_device()
+        self._bytes = self.workspace_bytes(64)   # one size for every call: memory a captured call holds is never exchanged for more
 
     def set_option(self, name, value):
         raise NotImplementedError("mixture-of-experts handles have no options")
@@ -496,7 +497,7 @@ class MoE(_Handle):
             experts = torch.empty((M, self.top_k), dtype=torch.int32, device=X.device) if experts is None else experts
             weights = torch.empty((M, self.top_k), dtype=torch.float32, device=X.device) if weights is None else weights
         pairs = (M, self.top_k)
-        ws = workspace if workspace is not None else self._own_workspace(M, X.device)
+        ws = workspace if workspace is not None else self._workspace(self._bytes, X.device)
         _check(lib().alg_moe_forward(self._h, X.data_ptr(), ldx, M, self._packed(W_router, "W_router", (self.D, self.E), self.router_type),
                                      None if select_bias is None else self._packed(select_bias, "select_bias", (self.E,), torch.float32),
                                      self._packed(W_gate_up, "W_gate_up", (self.E, self.D, 2 * self.F), torch.bfloat16),

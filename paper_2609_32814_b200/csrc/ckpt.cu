@@ -156,10 +156,16 @@ __device__ __forceinline__ uint64_t act2(uint64_t z, uint64_t *slope) {
     q = pair_fma(q, u, both(-1.1512017f));
     q = pair_fma(q, u, both(-0.99999309f));
     const uint64_t tail = exp2_of(q);
+    // z - u tail above 0, -u tail below: u for |z| is off by less than the tail there, and an infinite z stays what it is
+    auto above = [](float v) {   // max(v, 0), NaN for NaN
+      float r;
+      asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(v));
+      return r;
+    };
     float h0, h1;
     halves(pair_fma(tail, both(-1.f), both(0.5f)), h0, h1);
     *slope = pair_add(zphi, pair_add(pair(copysignf(h0, lo), copysignf(h1, hi)), both(0.5f)));
-    return pair_fma(pair(-fabsf(lo), -fabsf(hi)), tail, pair(fmaxf(lo, 0.f), fmaxf(hi, 0.f)));
+    return pair_fma(pair_mul(u, both(-1.f)), tail, pair(above(lo), above(hi)));
   }
   *slope = both(1.f);
   return z;

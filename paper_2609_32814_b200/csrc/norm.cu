@@ -281,6 +281,16 @@ alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const v
   Granules gr = {granule(*h)};
   if (sums && (!workspace || ((uintptr_t)workspace & 255u))) return ALG_ERR_INVALID_ARG;
   if (sums && workspace_bytes < sums_bytes(*h)) return ALG_ERR_WORKSPACE_TOO_SMALL;
+  const RowSpan ws = sums ? span(workspace, (int64_t)sums_bytes(*h), (int64_t)sums_bytes(*h), 1, 1) : span(nullptr, 0, 0, 1, 0);
+  for (int k = 0; k < 5; ++k) {   // a vector's gradient lies over nothing that is read, nor over another
+    if (!vectors_out[k]) continue;
+    const RowSpan out = span(vectors_out[k], D, D, 4, 1);
+    if (meet(out, ws)) return ALG_ERR_INVALID_ARG;
+    for (const float *v : vectors_in)
+      if (v && meet(out, span(v, D, D, 4, 1))) return ALG_ERR_INVALID_ARG;
+    for (int l = 0; l < k; ++l)
+      if (vectors_out[l] && meet(out, span(vectors_out[l], D, D, 4, 1))) return ALG_ERR_INVALID_ARG;
+  }
   NormArgs a = {};
   if (M > 0) {
     if ((pre && !Y) || !dR || pre != (dN != nullptr) || join != (F != nullptr) || (row || el) != (gate != nullptr) || (!pre && !dY)) return ALG_ERR_INVALID_ARG;
@@ -289,7 +299,6 @@ alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const v
                            row ? operand(gate, 1, 1, eb, M) : operand(gate, ldg, D, eb, M)};
     const Operand to[3] = {operand(dR, lddr, D, ex, M), operand(dF, lddf, D, eb, M),
                            row ? operand(dgate, 1, 1, eb, M) : operand(dgate, lddg, D, eb, M)};
-    const RowSpan ws = sums ? span(workspace, 0, (int64_t)sums_bytes(*h), 1, 1) : span(nullptr, 0, 0, 1, 0);
     for (int k = 0; k < 5; ++k) {
       if (!in[k].ok || meet(ws, in[k].s)) return ALG_ERR_INVALID_ARG;
       for (const float *v : vectors_out)

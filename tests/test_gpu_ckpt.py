@@ -171,6 +171,16 @@ def test_slope_against_differences(act):
     assert float(((hi - lo).double() / (2 * h) - dz.double()).abs().max()) <= h * h / 6 * 2.5 + 2 * 6 * 2.0 ** -22 / (2 * h)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+def test_values_that_are_not_finite_reach_the_activation(act, dtype):
+    z = torch.zeros(2, 64, device="cuda", dtype=DT[dtype])
+    z[0, 3], z[1, 40], z[1, 41] = math.nan, math.inf, 3.0
+    a, _ = binding.ActCheckpoint(64, act=act).forward(z, keep=False)
+    assert bool(a[0, 3].isnan()) and float(a[1, 40]) == math.inf and bool(torch.isfinite(a[1, 41]))
+    assert int(a.isnan().sum()) == 1 and int(a.isinf().sum()) == 1
+
+
 def test_far_tails_are_finite():
     z = torch.tensor([[-3e4, -200.0, -88.5, -20.0, 0.0, -0.0, 20.0, 88.5, 200.0, 3e4] + [0.0] * 22], device="cuda")
     for act in ("gelu", "gelu_tanh", "silu"):

@@ -217,6 +217,26 @@ def test_captured_calls_share_a_workspace_and_see_new_inputs():
         assert torch.equal(y2, layer.h.forward(x2, layer.Wr, layer.Wgu, layer.Wd))
 
 
+def test_a_captured_call_outlives_larger_calls_of_its_handle():
+    """The handle's own workspace is the same memory for every number of rows."""
+    layer = Layer(64, 256, 64, 10, 3)
+    args = (layer.Wr, layer.Wgu, layer.Wd)
+    x = layer.X[:1].clone()
+    want = layer.h.forward(x, *args)
+    y = torch.zeros_like(want)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        layer.h.forward(x, *args, out=y)
+    at = layer.h._ws.data_ptr()
+    layer.check(*layer.run())                       # 64 rows
+    assert layer.h._ws.data_ptr() == at
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
 def test_banks_past_32_bits():
     """Experts whose weights lie more than 2^32 bytes, and elements, into the banks."""
     e, d, f = 48, 4096, 11264

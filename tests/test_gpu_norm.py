@@ -358,6 +358,10 @@ def test_refusals():
     assert e.value.code == 3
     with pytest.raises(binding.AlgError):
         h.backward(x(), dY=x(), F=x(), gate=x())                      # a PRE handle needs dN
+    two = torch.ones(100, device="cuda")
+    for out in ({"scale": w}, {"scale": two[:64], "post_weight": two[36:]}):   # gradients over what is read, and over one another
+        with pytest.raises(binding.AlgError):
+            h.backward(x(), dY=x(), dN=x(), F=x(), gate=x(), scale=w, post_weight=torch.ones(64, device="cuda"), out=out)
     plain = binding.BlockNorm(64)
     with pytest.raises(binding.AlgError):
         plain.forward(x(), F=x())
