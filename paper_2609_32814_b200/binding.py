@@ -147,16 +147,21 @@ def _stream(stream=None):
 
 def _rows(t, what, M, cols, dtype, device):
     """The leading dimension of an M x cols operand with contiguous rows, of this dtype, on the handle's device."""
+    # (one test where all is well: these calls take a few microseconds, and have up to eight operands)
+    if t.shape == (M, cols) and t.dtype is dtype and t.get_device() == device:
+        ld, step = t.stride()
+        if M <= 1:
+            return cols if step == 1 or cols == 1 else _bad_rows(what)
+        return ld if ld >= cols and (step == 1 or cols == 1) else _bad_rows(what)
     if t.dim() != 2 or t.shape[0] != M or t.shape[1] != cols:
         raise ValueError(f"{what} must be {M} x {cols}, got {tuple(t.shape)}")
     if t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{what} must be on the handle's device, cuda:{device}")
-    ld, step = t.stride()
-    if (step != 1 and cols > 1) or (ld < cols and M > 1):
-        raise ValueError(f"{what} must have contiguous rows that do not overlap")
-    return ld if M > 1 else cols
+    raise ValueError(f"{what} must be on the handle's device, cuda:{device}")
+
+
+def _bad_rows(what):
+    raise ValueError(f"{what} must have contiguous rows that do not overlap")
 
 
 def _widths(w):
@@ -466,6 +471,7 @@ class MoE(_Handle):
                                     {"softmax": ALG_MOE_SOFTMAX, "sigmoid": ALG_MOE_SIGMOID}[score], int(bool(renormalise)), float(route_scale),
                                     _DTYPES[router_dtype]), "alg_moe_create")
         self._device = torch.cuda.current_device()
+        self._dev = torch.device("cuda", self._device)
         self._bytes = self.workspace_bytes(64)   # one size for every call: memory a captured call holds is never exchanged for more
 
     def set_option(self, name, value):
@@ -489,13 +495,13 @@ class MoE(_Handle):
         if M > 64:
             raise AlgError(2, "alg_moe_forward")
         if out is None:
-            out = torch.empty((M, self.D), dtype=out_dtype or X.dtype, device=X.device)
+            out = torch.empty_like(X) if out_dtype is None or out_dtype is X.dtype else torch.empty_like(X, dtype=out_dtype)
             ldo = self.D
         else:
             ldo = _rows(out, "out", M, self.D, out.dtype, self._device)
         if routing:
-            experts = torch.empty((M, self.top_k), dtype=torch.int32, device=X.device) if experts is None else experts
-            weights = torch.empty((M, self.top_k), dtype=torch.float32, device=X.device) if weights is None else weights
+            experts = torch.empty((M, self.top_k), dtype=torch.int32, device=self._dev) if experts is None else experts
+            weights = torch.empty((M, self.top_k), dtype=torch.float32, device=self._dev) if weights is None else weights
         pairs = (M, self.top_k)
         ws = workspace if workspace is not None else self._workspace(self._bytes, X.device)
         _check(lib().alg_moe_forward(self._h, X.data_ptr(), ldx, M, self._packed(W_router, "W_router", (self.D, self.E), self.router_type),
@@ -523,6 +529,7 @@ class BlockNorm(_Handle):
     def __init__(self, D, kind="rms", join=False, pre=True, post=False, gate=None, gate_act=None, eps=1e-6, dtype="bf16", stream_dtype="bf16"):
         super().__init__()
         self.D, self.join, self.pre, self.post, self.gate = int(D), bool(join), bool(pre), bool(post), gate
+        self._shape = (self.D,)
         self.stream_type, self.type = (torch.float32 if _DTYPES[t] == ALG_F32 else torch.bfloat16 for t in (stream_dtype, dtype))
         flags = ((ALG_NORM_JOIN if join else 0) | (ALG_NORM_PRE if pre else 0) | (ALG_NORM_POST if post else 0) |
                  {None: 0, "row": ALG_NORM_GATE_ROW, "element": ALG_NORM_GATE_ELEMENT}[gate] |
@@ -530,6 +537,7 @@ class BlockNorm(_Handle):
         _check(lib().alg_norm_create(ctypes.byref(self._h), self.D, {"rms": ALG_NORM_RMS, "layer": ALG_NORM_LAYER}[kind], flags, float(eps),
                                      _DTYPES[stream_dtype], _DTYPES[dtype]), "alg_norm_create")
         self._device = torch.cuda.current_device()
+        self._dev = torch.device("cuda", self._device)
         out = ctypes.c_size_t()
         _check(lib().alg_norm_workspace_bytes(self._h, ctypes.byref(out)), "alg_norm_workspace_bytes")
         self._bytes = out.value
@@ -543,13 +551,13 @@ class BlockNorm(_Handle):
 
     def _matrix(self, t, what, M, dtype):
         """(address, leading dimension) of an operand."""
-        if t is None:
-            return None, 0
-        return t.data_ptr(), _rows(t, what, M, self.D, dtype, self._device)
+        return (None, 0) if t is None else (t.data_ptr(), _rows(t, what, M, self.D, dtype, self._device))
 
     def _gate(self, t, what, M):
-        if t is None or self.gate != "row":
-            return self._matrix(t, what, M, self.type)
+        if t is None:
+            return None, 0
+        if self.gate != "row":
+            return t.data_ptr(), _rows(t, what, M, self.D, self.type, self._device)
         if t.shape != (M,) or t.dtype is not self.type or t.get_device() != self._device or (M > 1 and t.stride(0) != 1):
             raise ValueError(f"{what} must hold {M} packed {self.type} values on the handle's device")
         return t.data_ptr(), 0
@@ -557,60 +565,80 @@ class BlockNorm(_Handle):
     def _vector(self, t, what):
         if t is None:
             return None
-        if t.shape != (self.D,) or t.dtype is not torch.float32 or t.get_device() != self._device or (self.D > 1 and t.stride(0) != 1):
+        if t.shape != self._shape or t.dtype is not torch.float32 or t.get_device() != self._device or (t.stride(0) != 1 and self.D > 1):
             raise ValueError(f"{what} must hold {self.D} packed float32 values on the handle's device")
         return t.data_ptr()
 
     def _new(self, M, dtype):
-        return torch.empty((M, self.D), dtype=dtype, device=f"cuda:{self._device}")
+        return torch.empty((M, self.D), dtype=dtype, device=self._dev)
 
     def forward(self, R, F=None, gate=None, post_weight=None, post_bias=None, scale=None, alpha=1.0, pre_weight=None, pre_bias=None, out=None,
                 normed=None, stream=None):
         """(Y, N); Y is R without ``join``, N is None without ``pre``."""
-        M = R.shape[0]
+        M, D, dev, st, dt, vec = R.shape[0], self.D, self._device, self.stream_type, self.type, self._vector
         if self.join and out is None:
-            out = self._new(M, self.stream_type)
+            out, ldo = torch.empty_like(R), D
+        else:
+            ldo = 0 if out is None else _rows(out, "out", M, D, st, dev)
         if self.pre and normed is None:
-            normed = self._new(M, self.type)
-        _check(lib().alg_norm_forward(self._h, *self._matrix(R, "R", M, self.stream_type), *self._matrix(F, "F", M, self.type),
-                                      *self._gate(gate, "gate", M), self._vector(post_weight, "post_weight"), self._vector(post_bias, "post_bias"),
-                                      self._vector(scale, "scale"), alpha, self._vector(pre_weight, "pre_weight"),
-                                      self._vector(pre_bias, "pre_bias"), M, *self._matrix(out, "out", M, self.stream_type),
-                                      *self._matrix(normed, "normed", M, self.type), _stream(stream)), "alg_norm_forward")
+            normed, ldn = torch.empty_like(R) if st is dt else torch.empty_like(R, dtype=dt), D
+        else:
+            ldn = 0 if normed is None else _rows(normed, "normed", M, D, dt, dev)
+        g, ldg = self._gate(gate, "gate", M)
+        code = lib().alg_norm_forward(
+            self._h, R.data_ptr(), _rows(R, "R", M, D, st, dev), None if F is None else F.data_ptr(), 0 if F is None else _rows(F, "F", M, D, dt, dev),
+            g, ldg, vec(post_weight, "post_weight"), vec(post_bias, "post_bias"), vec(scale, "scale"), alpha, vec(pre_weight, "pre_weight"),
+            vec(pre_bias, "pre_bias"), M, None if out is None else out.data_ptr(), ldo, None if normed is None else normed.data_ptr(), ldn,
+            _stream(stream))
+        if code:
+            _check(code, "alg_norm_forward")
         return (out if self.join else R), normed
 
     def backward(self, Y, dY=None, dN=None, F=None, gate=None, post_weight=None, post_bias=None, scale=None, alpha=1.0, pre_weight=None,
                  pre_bias=None, want=None, out=None, workspace=None, stream=None):
         """The gradients, by name: "R", "F", "gate" and those of the vectors given.  ``want``: the names to compute (R always is) instead of
         all of these; ``out``: tensors to write some of them to."""
-        M = Y.shape[0]
-        given = {"post_weight": post_weight, "post_bias": post_bias, "scale": scale, "pre_weight": pre_weight, "pre_bias": pre_bias}
-        if want is None:
-            want = [k for k, v in given.items() if v is not None] + ["F", "gate"][:(1 + (self.gate is not None)) if self.join else 0]
+        M, D, dev, st, dt, vec = Y.shape[0], self.D, self._device, self.stream_type, self.type, self._vector
+        ldy = _rows(Y, "Y", M, D, st, dev)
         got = dict(out) if out else {}
-        for k in ("R", *want):
-            if k in got:
-                continue
-            if k in given:
-                got[k] = torch.empty((self.D,), dtype=torch.float32, device=f"cuda:{self._device}")
-            elif k == "gate" and self.gate == "row":
-                got[k] = torch.empty((M,), dtype=self.type, device=f"cuda:{self._device}")
-            elif k in ("R", "F", "gate"):
-                got[k] = self._new(M, self.stream_type if k == "R" else self.type)
-            else:
-                raise ValueError(f"no gradient is called {k}")
+        if "R" not in got:
+            got["R"] = torch.empty_like(Y)
+        names = ("post_weight", "post_bias", "scale", "pre_weight", "pre_bias")
+        given = (post_weight, post_bias, scale, pre_weight, pre_bias)
+        if want is None:
+            for k, v in zip(names, given):
+                if v is not None and k not in got:
+                    got[k] = torch.empty_like(v)
+            if self.join and F is not None:
+                if "F" not in got:
+                    got["F"] = torch.empty_like(F)
+                if gate is not None and "gate" not in got:
+                    got["gate"] = torch.empty_like(gate)
+        else:
+            for k in want:
+                if k in got:
+                    continue
+                if k in names:
+                    got[k] = torch.empty((D,), dtype=torch.float32, device=self._dev)
+                elif k == "gate" and self.gate == "row":
+                    got[k] = torch.empty((M,), dtype=dt, device=self._dev)
+                elif k in ("F", "gate"):
+                    got[k] = self._new(M, dt)
+                else:
+                    raise ValueError(f"no gradient is called {k}")
+        to = [got.get(k) for k in names]
         ws = None
-        if any(k in got for k in given):
+        if any(t is not None for t in to):
             ws = workspace if workspace is not None else self._workspace(self._bytes, Y.device)
-        vec = [self._vector(got.get(k), f"the gradient of {k}") for k in given]
-        _check(lib().alg_norm_backward(self._h, *self._matrix(Y, "Y", M, self.stream_type), *self._matrix(dY, "dY", M, self.stream_type),
-                                       *self._matrix(dN, "dN", M, self.type), *self._matrix(F, "F", M, self.type), *self._gate(gate, "gate", M),
-                                       self._vector(post_weight, "post_weight"), self._vector(post_bias, "post_bias"),
-                                       self._vector(scale, "scale"), alpha, self._vector(pre_weight, "pre_weight"), M,
-                                       *self._matrix(got["R"], "the gradient of R", M, self.stream_type),
-                                       *self._matrix(got.get("F"), "the gradient of F", M, self.type),
-                                       *self._gate(got.get("gate"), "the gradient of gate", M), *vec, _ptr(ws), 0 if ws is None else ws.numel(),
-                                       _stream(stream)), "alg_norm_backward")
+        rows = self._matrix
+        code = lib().alg_norm_backward(
+            self._h, Y.data_ptr(), ldy, *rows(dY, "dY", M, st), *rows(dN, "dN", M, dt), *rows(F, "F", M, dt), *self._gate(gate, "gate", M),
+            vec(post_weight, "post_weight"), vec(post_bias, "post_bias"), vec(scale, "scale"), alpha, vec(pre_weight, "pre_weight"), M,
+            *rows(got["R"], "the gradient of R", M, st), *rows(got.get("F"), "the gradient of F", M, dt),
+            *self._gate(got.get("gate"), "the gradient of gate", M), *[None if t is None else vec(t, "a vector's gradient") for t in to], _ptr(ws),
+            0 if ws is None else ws.numel(), _stream(stream))
+        if code:
+            _check(code, "alg_norm_backward")
         return got
 
     def last_status(self, stream=None) -> int:
@@ -631,6 +659,7 @@ class ActCheckpoint(_Handle):
         self.cols, self.wide = int(cols), int(cols) * (2 if gated else 1)
         _check(lib().alg_ckpt_create(ctypes.byref(self._h), self.cols, _Q8[fmt], _CKPT_ACTS[act], int(bool(gated))), "alg_ckpt_create")
         self._device = torch.cuda.current_device()
+        self._dev = torch.device("cuda", self._device)
         out = ctypes.c_size_t()
         _check(lib().alg_ckpt_row_bytes(self._h, ctypes.byref(out)), "alg_ckpt_row_bytes")
         self.row_bytes = out.value
@@ -640,17 +669,16 @@ class ActCheckpoint(_Handle):
 
     def new(self, M):
         """Memory for M records."""
-        return torch.empty((M, self.row_bytes), dtype=torch.uint8, device=f"cuda:{self._device}")
+        return torch.empty((M, self.row_bytes), dtype=torch.uint8, device=self._dev)
 
     def _records(self, ckpt, M):
         if _rows(ckpt, "the checkpoint", M, self.row_bytes, torch.uint8, self._device) != self.row_bytes:
             raise ValueError("the checkpoint's records must be packed")
         return ckpt.data_ptr()
 
-    def _out(self, out, what, M, cols, dtype):
+    def _out(self, out, what, M, cols, dtype, like=None):
         if out is None:
-            out = torch.empty((M, cols), dtype=dtype, device=f"cuda:{self._device}")
-            return out, cols
+            return (torch.empty((M, cols), dtype=dtype, device=self._dev) if like is None else torch.empty_like(like)), cols
         return out, _rows(out, what, M, cols, dtype, self._device)
 
     def store(self, X, out=None, stream=None):
@@ -672,7 +700,7 @@ class ActCheckpoint(_Handle):
         """(A, checkpoint of Z); keep=False: (A, None), nothing is kept."""
         M = Z.shape[0]
         ldz = _rows(Z, "Z", M, self.wide, Z.dtype, self._device)
-        out, ldo = self._out(out, "out", M, self.cols, Z.dtype)
+        out, ldo = self._out(out, "out", M, self.cols, Z.dtype, Z if self.wide == self.cols else None)
         if keep and ckpt is None:
             ckpt = self.new(M)
         _check(lib().alg_ckpt_act_forward(self._h, Z.data_ptr(), ldz, M, out.data_ptr(), ldo, _DTYPES[Z.dtype],
@@ -683,8 +711,8 @@ class ActCheckpoint(_Handle):
         """(dZ, A) from the checkpoint of Z and the gradient of A.  ``again``: a tensor for A, True for a new one, False for none."""
         M = dA.shape[0]
         ldd = _rows(dA, "dA", M, self.cols, dA.dtype, self._device)
-        out, ldo = self._out(out, "out", M, self.wide, dA.dtype)
-        A, lda = (None, 0) if again is False or again is None else self._out(None if again is True else again, "again", M, self.cols, dA.dtype)
+        out, ldo = self._out(out, "out", M, self.wide, dA.dtype, dA if self.wide == self.cols else None)
+        A, lda = (None, 0) if again is False or again is None else self._out(None if again is True else again, "again", M, self.cols, dA.dtype, dA)
         _check(lib().alg_ckpt_act_backward(self._h, self._records(ckpt, M), dA.data_ptr(), ldd, M, out.data_ptr(), ldo, _ptr(A), lda,
                                            _DTYPES[dA.dtype], _stream(stream)), "alg_ckpt_act_backward")
         return out, A
