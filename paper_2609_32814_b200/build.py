@@ -16,8 +16,8 @@ OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libalgproj.so")
 # (the ones that take long first)
 SOURCES = ["proj_big.cu", "proj_tc.cu", "norm_backward_any_wide.cu", "moe.cu", "ffn_decode.cu", "norm_forward_any.cu", "norm_backward_rms_bf16.cu",
-           "norm_backward_rms_f32.cu", "norm_forward_bf16.cu", "norm_forward_f32.cu", "row_decode.cu", "norm_backward_layer_bf16.cu",
-           "norm_backward_layer_f32.cu", "ckpt.cu", "norm_backward_any.cu", "decode.cu", "proj_split.cu", "proj_simt.cu", "proj_tc2.cu", "bucket.cu",
+           "norm_backward_rms_f32.cu", "norm_forward_bf16.cu", "norm_forward_f32.cu", "row_decode.cu", "norm_backward_layer_wide_bf16.cu", "norm_backward_layer_wide_f32.cu",
+           "norm_backward_layer_bf16.cu", "norm_backward_layer_f32.cu", "ckpt.cu", "norm_backward_any.cu", "decode.cu", "proj_split.cu", "proj_simt.cu", "proj_tc2.cu", "bucket.cu",
            "api.cu", "norm.cu", "static_ws.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]

@@ -61,10 +61,11 @@ __global__ void __launch_bounds__(32 * kSlices) norm_sums_kernel(const SumsArgs 
   if (y == 3 && a.d_post_b) a.d_post_b[c] = scale * r;
 }
 
+// Places before a row's first column in its first granule, at most.
+int most_off(const NormArgs &a) { return a.period > 1 || a.off ? 7 : 0; }
 // Threads of a row, rows a CTA works on at once, rows on their way; the grid.
 int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool full, bool back, size_t *smem) {
-  const int most_off = a.period > 1 || a.off ? 7 : 0;   // a shifted row's places
-  a.T = (a.D + most_off + 256 * v - 1) / (256 * v) * 32;
+  a.T = (a.D + most_off(a) + 256 * v - 1) / (256 * v) * 32;
   a.stage_bytes = 0;
   for (int k = 0; k < kOps; ++k) {
     a.at[k] = a.stage_bytes;
@@ -72,9 +73,11 @@ int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool full, bool back, si
     if (a.op[k]) a.stage_bytes += (int)((a.bytes[k] + 30) / 16 * 16);   // (a row off 16 bytes brings up to 15 on either side)
   }
   const size_t stage = a.stage_bytes;
-  const int kept = ((a.flags & ALG_NORM_JOIN ? 1 : 0) + (a.flags & ALG_NORM_PRE ? 1 : 0)) * (full ? 2 : 1);
-  a.vectors = kept * a.T * v * 32;
-  if (a.vectors > kVectorBytes) a.vectors = 0;   // (only rows of sixteen columns a thread have as many)
+  a.kept = (a.flags & ALG_NORM_JOIN ? full ? 3 : 1 : 0) | (a.flags & ALG_NORM_PRE ? full && !back ? 12 : 4 : 0);
+  a.vectors = __builtin_popcount(a.kept) * a.T * v * 32;
+  // kept as long as a row's stage fits beside them, which only fp32 rows past 4096 columns may not (LayerNorm of 8000 x 8192 bf16, where the vectors
+  // leave one stage: 140 us forward and 320 backward, from L2 at their use 496 and 845)
+  if (a.vectors + stage > (size_t)kBudget) a.vectors = 0;
   const size_t budget = (size_t)kBudget - a.vectors;
   int groups = kThreads / a.T;
   if (groups > kMaxGroups) groups = kMaxGroups;
@@ -99,7 +102,7 @@ int shape_rows(const alg_norm_s &h, NormArgs &a, int v, bool full, bool back, si
 int granule(const alg_norm_s &h) { return h.stream_dtype == ALG_BF16 && h.dtype == ALG_BF16 ? 8 : 4; }
 // Columns a thread has, in eights.  The sums of LayerNorm's backward pass (four a column) leave registers for eight columns; all else takes
 // sixteen, which halves what a row costs each thread besides its columns (32768 x 4096 forward 274 against 265 us, gradients of 8003 x 1024 47 against 40).
-int eights(bool back, bool full, int D) { return back && full && D <= kNarrow ? 1 : 2; }
+int eights(bool back, bool full, const NormArgs &a) { return back && full && a.D + most_off(a) <= kNarrow ? 1 : 2; }
 
 // *full: LayerNorm or biases (set here; the caller asks for gradients of biases).  Kernels with their form as a constant serve bf16 F, gate and N, with dY and all gradients in the backward pass, LayerNorm (with or without biases) or RMS norm without biases, whose
 // folded vectors fit.  alike: the matrices lie off their granules alike; on16: they and the vectors lie on 16 bytes.
@@ -107,28 +110,30 @@ template <bool BACK>
 cudaError_t launch_norm(const alg_norm_s &h, NormArgs &a, bool alike, bool on16, bool *full, int *grid, cudaStream_t st) {
   size_t smem = 0;
   *full = *full || a.layer || a.post_b || a.pre_b;
-  const int v = eights(BACK, *full, a.D);
+  if (a.D + most_off(a) > 2 * kNarrow) alike = false, a.off = a.ld_off = 0, a.period = 1;   // (more than the threads of a CTA hold)
+  const int v = eights(BACK, *full, a);
   const bool gated = a.flags & (ALG_NORM_GATE_ROW | ALG_NORM_GATE_ELEMENT), join = a.flags & ALG_NORM_JOIN;
   bool form = alike && (a.flags & (ALG_NORM_PRE | ALG_NORM_POST)) && h.dtype == ALG_BF16 && *full == (a.layer != 0);
-  if (BACK) form = form && a.op[kT] && (!join || a.out) && (!gated || a.dg) && v == (a.layer ? 1 : 2);
+  if (BACK) form = form && a.op[kT] && (!join || a.out) && (!gated || a.dg) && (a.layer || v == 2);
   if (form) {
     *grid = shape_rows(h, a, v, *full, BACK, &smem);
     form = a.vectors > 0;
   }
   if (form) {
-    const int gate = !gated ? kGateNone : a.flags & ALG_NORM_GATE_ROW ? kGateRow : kGateElement;
+    const int gate = !gated ? kGateNone : a.flags & ALG_NORM_GATE_ROW ? kGateRow : a.flags & ALG_NORM_GATE_SIGMOID ? kGateSigmoid : kGateElement;
     const int f = (a.flags & ALG_NORM_PRE ? kFormPre : 0) | (a.flags & ALG_NORM_POST ? kFormPost : 0) | (join ? kFormJoin : 0);
     const bool bf16 = h.stream_dtype == ALG_BF16;
     if constexpr (BACK) {
-      auto *launch = a.layer ? (bf16 ? launch_norm_backward_layer_bf16 : launch_norm_backward_layer_f32)
-                             : (bf16 ? launch_norm_backward_rms_bf16 : launch_norm_backward_rms_f32);
+      auto *launch = !a.layer ? (bf16 ? launch_norm_backward_rms_bf16 : launch_norm_backward_rms_f32)
+                     : v == 1 ? (bf16 ? launch_norm_backward_layer_bf16 : launch_norm_backward_layer_f32)
+                              : (bf16 ? launch_norm_backward_layer_wide_bf16 : launch_norm_backward_layer_wide_f32);
       return launch(a, f + kFormGate * gate, on16, *grid, smem, st);
     } else {
       return (bf16 ? launch_norm_forward_bf16 : launch_norm_forward_f32)(a, f + kFormGate * gate, a.layer, on16, *grid, smem, st);
     }
   }
   *full = true;
-  const int w = eights(BACK, true, a.D);
+  const int w = eights(BACK, true, a);
   *grid = shape_rows(h, a, w, true, BACK, &smem);
   const bool exact = on16 && a.D % granule(h) == 0;
   const int types = (h.stream_dtype == ALG_F32 ? 2 : 0) + (h.dtype == ALG_F32 ? 1 : 0);

@@ -1,7 +1,7 @@
 // A block's border: Y = R + alpha * scale * g * (norm(F) * w + b) and N = norm(Y) * w' + b', and the gradients of both.
 //
 // A row is D <= 8192 features, read and written once: bound by HBM, if the arithmetic is kept short (72 instructions a value
-// took twice the time of the bytes).  A group of T threads takes a row at a time, eight columns a thread (16 past 4096); the rows of its
+// took twice the time of the bytes).  A group of T threads takes a row at a time, sixteen columns a thread (eight in the gradients of LayerNorm to 4096); the rows of its
 // operands come into shared memory by the bulk copy engine, `stages` rows ahead, so that what is in flight does not depend on how
 // many registers the arithmetic takes.  Vectors are folded once a CTA (alpha * scale * post_weight, ...) and kept in shared memory; arithmetic is on
 // pairs; up to four sums cross the group in one exchange.
@@ -30,14 +30,15 @@ cudaError_t launch_norm_forward_bf16(NormArgs &a, int form, bool layer, bool on1
 cudaError_t launch_norm_forward_f32(NormArgs &a, int form, bool layer, bool on16, int grid, size_t smem, cudaStream_t st);
 cudaError_t launch_norm_backward_rms_bf16(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
 cudaError_t launch_norm_backward_layer_bf16(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_layer_wide_bf16(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
 cudaError_t launch_norm_backward_rms_f32(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
 cudaError_t launch_norm_backward_layer_f32(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
+cudaError_t launch_norm_backward_layer_wide_f32(NormArgs &a, int form, bool on16, int grid, size_t smem, cudaStream_t st);
 
 
 constexpr int kMaxStages = 4;
 constexpr int kMaxGroups = 15;             // named barriers 1 .. 15
 constexpr int kBudget = 224 * 1024;        // shared memory of a CTA for its vectors and rows
-constexpr int kVectorBytes = 64 * 1024;    // folded vectors that are kept in shared memory
 constexpr int kNarrow = 4096;              // widest row of eight columns a thread
 constexpr int kThreads = 512;              // of a CTA, at most
 constexpr int kSums = 4;                   // column sums: dN * v, dN, P, Q
@@ -57,7 +58,8 @@ struct NormArgs {
   uint8_t *y, *out;             // forward: Y, N; backward: dR, dF
   uint8_t *dg;                  // backward: gradient of the gate
   uint32_t pitch_y, pitch_out, pitch_dg;
-  int vectors;                  // bytes of the folded vectors in shared memory; 0: read where they lie
+  int kept;                     // the folded vectors a kernel reads, a bit each
+  int vectors;                  // their bytes in shared memory; 0: read where they lie
   float *part;                  // [CTAs][kSums][D]
   int *status;
   long long wait_limit;
@@ -66,7 +68,9 @@ struct NormArgs {
 // The form of a call: what it does, as a constant of a kernel (kAny: found out at run time, with every branch that costs: gradients of
 // 16384 x 4096 rows 467 us against 320).
 enum { kFormPre = 1, kFormPost = 2, kFormJoin = 4, kFormGate = 8, kAny = -1 };   // + kFormGate * gate
-enum { kGateNone, kGateRow, kGateElement };   // (whether through a sigmoid is asked at run time)
+// gate of each element: whether through a sigmoid is part of the form, asked at run time it kept registers alive that the backward pass
+// spilled (283 us where the constant takes 271, 16384 x 8192 bf16); a row's gate asks at run time
+enum { kGateNone, kGateRow, kGateElement, kGateSigmoid };
 
 namespace {
 
@@ -240,13 +244,12 @@ struct Vectors {
 };
 // Which of them a kernel keeps; all threads, before the rows.
 template <int MAP, int V>
-__device__ __forceinline__ Vectors fold_vectors(const NormArgs &a, uint8_t *smem, bool full) {
+__device__ __forceinline__ Vectors fold_vectors(const NormArgs &a, uint8_t *smem) {
   Vectors vec = {{nullptr, nullptr, nullptr, nullptr}};
   float *to = (float *)(smem + kRowsAt);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const bool used = (k < 2 ? a.flags & ALG_NORM_JOIN : a.flags & ALG_NORM_PRE) && (full || !(k & 1));
-    if (!used || !a.vectors) continue;
+    if (!(a.kept >> k & 1) || !a.vectors) continue;
     const int shift = shift_of<MAP>(a);
     if (MAP & kExact) {
 #pragma unroll 4
@@ -305,7 +308,7 @@ __device__ __forceinline__ uint32_t first_row(const NormArgs &a, int g) { return
 // The loop over a group's rows: body(row, stage, release); release() once the row's operands are read and a barrier of the group has
 // followed.
 template <int MAP, int V, typename XT, typename BT, typename Body>
-__device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vectors *vec, bool full, Body body) {
+__device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vectors *vec, Body body) {
   const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
   uint8_t *const rows = smem + kRowsAt + a.vectors + g * a.stages * a.stage_bytes;
   const uint32_t bar = tc::smem_u32(smem) + g * a.stages * 8, rows_at = tc::smem_u32(rows);
@@ -319,7 +322,7 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
   const uint32_t first = first_row(a, g), step = row_step(a);
   for (int s = 0; s < a.stages; ++s)
     if (first + s * step < a.M) issue_row<!(MAP & kExact)>(a, rows_at + s * a.stage_bytes, bar + 8 * s, first + s * step, t);
-  *vec = fold_vectors<MAP, V>(a, smem, full);
+  *vec = fold_vectors<MAP, V>(a, smem);
   __syncthreads();
   int s = 0;
   uint32_t parity = 0;
@@ -363,12 +366,12 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const NormArg
   constexpr int gate_of = any ? 0 : FORM / kFormGate;
   const bool pre = any ? a.flags & ALG_NORM_PRE : FORM & kFormPre, join = any ? a.flags & ALG_NORM_JOIN : FORM & kFormJoin;
   const bool post = any ? a.flags & ALG_NORM_POST : FORM & kFormPost, layer = any ? FULL && a.layer : FULL;
-  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of == kGateElement;
-  const bool sig = (any || gate_of) && a.flags & ALG_NORM_GATE_SIGMOID;
+  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of >= kGateElement;
+  const bool sig = any || gate_of == kGateRow ? a.flags & ALG_NORM_GATE_SIGMOID : gate_of == kGateSigmoid;
   int turn = 0;
   Vectors vec;
   float gate_ahead = 0.f;
-  each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
+  each_row<MAP, V, XT, BT>(a, smem, &vec, [&](uint32_t row, const uint8_t *st, auto release) {
     F8 y[V], f[V], q[V];
     bool held = true;
     const float gate = gate_row ? next_gate((const BT *)a.gate, row, a, gate_ahead) : 1.f;
@@ -447,8 +450,8 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
   constexpr int gate_of = any ? 0 : FORM / kFormGate;
   const bool pre = any ? a.flags & ALG_NORM_PRE : FORM & kFormPre, join = any ? a.flags & ALG_NORM_JOIN : FORM & kFormJoin;
   const bool post = any ? a.flags & ALG_NORM_POST : FORM & kFormPost, layer = any ? FULL && a.layer : FULL;
-  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of == kGateElement;
-  const bool sig = (any || gate_of) && a.flags & ALG_NORM_GATE_SIGMOID;
+  const bool gate_row = any ? a.flags & ALG_NORM_GATE_ROW : gate_of == kGateRow, gate_el = any ? a.flags & ALG_NORM_GATE_ELEMENT : gate_of >= kGateElement;
+  const bool sig = any || gate_of == kGateRow ? a.flags & ALG_NORM_GATE_SIGMOID : gate_of == kGateSigmoid;
   // (a form that is a constant comes with dY and with every gradient wanted)
   const bool has_dy = any ? a.op[kT] != nullptr : true, to_f = any ? a.out != nullptr : true, to_gate = any ? a.dg != nullptr : true;
   F8 sum[kSums][V];
@@ -459,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
   int turn = 0;
   Vectors vec;
   float gate_ahead = 0.f;
-  each_row<MAP, V, XT, BT>(a, smem, &vec, FULL, [&](uint32_t row, const uint8_t *st, auto release) {
+  each_row<MAP, V, XT, BT>(a, smem, &vec, [&](uint32_t row, const uint8_t *st, auto release) {
     // a row of eight columns a thread stays in registers, a wider one is read from its stage as needed
     F8 hx, hn, hf, hh;   // (hh: dN * pre_weight)
     auto x_of = [&](int v) { return V == 1 ? hx : cols.load(staged<XT, MAP>(a, st, kX, row, shift), v); };
@@ -658,7 +661,8 @@ cudaError_t launch_gate(NormArgs &a, int gate, bool on16, int grid, size_t smem,
   switch (gate) {
     case kGateNone: return launch_form<BACK, XT, V, LAYER, BASE>(a, on16, grid, smem, st);
     case kGateRow: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateRow>(a, on16, grid, smem, st);
-    default: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateElement>(a, on16, grid, smem, st);
+    case kGateElement: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateElement>(a, on16, grid, smem, st);
+    default: return launch_form<BACK, XT, V, LAYER, BASE + kFormGate * kGateSigmoid>(a, on16, grid, smem, st);
   }
 }
 template <bool BACK, typename XT, int V, bool LAYER>

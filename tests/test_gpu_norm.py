@@ -194,7 +194,9 @@ def test_border_and_its_gradients(form, dtype, stream, m, d, pitch, at):
 @pytest.mark.parametrize("kind,dtype,stream,m,d", [("rms", "bf16", "bf16", 1999, 768), ("layer", "bf16", "f32", 700, 2048), ("rms", "f32", "f32", 300, 4096),
                                                    ("layer", "f32", "f32", 310, 8192), ("rms", "bf16", "bf16", 450, 7168), ("layer", "bf16", "bf16", 160, 4104),
                                                    ("rms", "bf16", "f32", 155, 5003), ("layer", "bf16", "bf16", 2001, 96), ("rms", "bf16", "bf16", 1201, 1002), ("layer", "bf16", "f32", 903, 2047),
-                                                   ("rms", "bf16", "bf16", 333, 4097)])
+                                                   ("rms", "bf16", "bf16", 333, 4097), ("layer", "bf16", "bf16", 320, 8192), ("layer", "bf16", "f32", 301, 5003),
+                                                   ("layer", "bf16", "f32", 299, 8192), ("layer", "bf16", "bf16", 170, 4091), ("layer", "f32", "f32", 150, 4095),
+                                                   ("rms", "bf16", "bf16", 163, 8191), ("layer", "bf16", "f32", 161, 8186), ("layer", "bf16", "bf16", 320, 8184)])
 def test_many_rows(kind, dtype, stream, m, d):
     """More rows than a grid takes at once, every width of a thread's share, stages that wrap."""
     b = Border(m, d, kind, True, True, "element", True, True, dtype, stream)
