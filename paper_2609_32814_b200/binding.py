@@ -601,42 +601,43 @@ class BlockNorm(_Handle):
         M, D, dev, st, dt, vec = Y.shape[0], self.D, self._device, self.stream_type, self.type, self._vector
         ldy = _rows(Y, "Y", M, D, st, dev)
         got = dict(out) if out else {}
-        if "R" not in got:
-            got["R"] = torch.empty_like(Y)
         names = ("post_weight", "post_bias", "scale", "pre_weight", "pre_bias")
         given = (post_weight, post_bias, scale, pre_weight, pre_bias)
-        if want is None:
-            for k, v in zip(names, given):
-                if v is not None and k not in got:
-                    got[k] = torch.empty_like(v)
-            if self.join and F is not None:
-                if "F" not in got:
-                    got["F"] = torch.empty_like(F)
-                if gate is not None and "gate" not in got:
-                    got["gate"] = torch.empty_like(gate)
+        read = [vec(v, k) for v, k in zip(given, names)]
+        rows, gates = self._matrix, self._gate
+        f_at, g_at = rows(F, "F", M, dt), gates(gate, "gate", M)
+        # (what is allocated here needs no checks, and lies as the operand it is the gradient of: with contiguous rows)
+        if "R" in got:
+            r_to = rows(got["R"], "the gradient of R", M, st)
         else:
-            for k in want:
-                if k in got:
-                    continue
-                if k in names:
-                    got[k] = torch.empty((D,), dtype=torch.float32, device=self._dev)
-                elif k == "gate" and self.gate == "row":
-                    got[k] = torch.empty((M,), dtype=dt, device=self._dev)
-                elif k in ("F", "gate"):
-                    got[k] = self._new(M, dt)
-                else:
-                    raise ValueError(f"no gradient is called {k}")
-        to = [got.get(k) for k in names]
+            got["R"] = t = torch.empty_like(Y)
+            r_to = t.data_ptr(), D
+        if want is None:
+            want = [k for k, at in zip(names, read) if at is not None]
+            if self.join and F is not None:
+                want += ("F",) if gate is None else ("F", "gate")
+        own = {}
+        for k in want:
+            if k in got:
+                continue
+            if k in names:
+                t = torch.empty((D,), dtype=torch.float32, device=self._dev) if pre_weight is None else torch.empty_like(pre_weight)
+            elif k == "F":
+                t = self._new(M, dt) if F is None else torch.empty_like(F)
+            elif k == "gate":
+                t = torch.empty((M,) if self.gate == "row" else (M, D), dtype=dt, device=self._dev) if gate is None else torch.empty_like(gate)
+            else:
+                raise ValueError(f"no gradient is called {k}")
+            got[k], own[k] = t, t.data_ptr()
+        f_to = (own["F"], D) if "F" in own else rows(got.get("F"), "the gradient of F", M, dt)
+        g_to = (own["gate"], D) if "gate" in own else gates(got.get("gate"), "the gradient of gate", M)
+        to = [own[k] if k in own else vec(got.get(k), "the gradient of " + k) for k in names]
         ws = None
-        if any(t is not None for t in to):
+        if to != [None] * 5:
             ws = workspace if workspace is not None else self._workspace(self._bytes, Y.device)
-        rows = self._matrix
         code = lib().alg_norm_backward(
-            self._h, Y.data_ptr(), ldy, *rows(dY, "dY", M, st), *rows(dN, "dN", M, dt), *rows(F, "F", M, dt), *self._gate(gate, "gate", M),
-            vec(post_weight, "post_weight"), vec(post_bias, "post_bias"), vec(scale, "scale"), alpha, vec(pre_weight, "pre_weight"), M,
-            *rows(got["R"], "the gradient of R", M, st), *rows(got.get("F"), "the gradient of F", M, dt),
-            *self._gate(got.get("gate"), "the gradient of gate", M), *[None if t is None else vec(t, "a vector's gradient") for t in to], _ptr(ws),
-            0 if ws is None else ws.numel(), _stream(stream))
+            self._h, Y.data_ptr(), ldy, *rows(dY, "dY", M, st), *rows(dN, "dN", M, dt), *f_at, *g_at, *read[:3], alpha, read[3], M, *r_to, *f_to,
+            *g_to, *to, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream))
         if code:
             _check(code, "alg_norm_backward")
         return got
