@@ -133,7 +133,10 @@ __device__ __forceinline__ uint64_t act2(uint64_t z, uint64_t *slope) {
   }
   if (ACT == ALG_ACT_GELU_TANH) {   // (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), 2u = 2k z (1 + c z^2)
     const float k2 = 2.f * 0.7978845608028654f, c = 0.044715f;
-    const uint64_t zz = pair_mul(z, z), u = pair_mul(z, pair_fma(zz, both(-log2e * k2 * c), both(-log2e * k2)));
+    // (squares that would be infinite: 0 * infinity in the slope; far behind where 1 - p is 0)
+    float s0, s1;
+    halves(pair_mul(z, z), s0, s1);
+    const uint64_t zz = pair(fminf(s0, 1e30f), fminf(s1, 1e30f)), u = pair_mul(z, pair_fma(zz, both(-log2e * k2 * c), both(-log2e * k2)));
     const uint64_t p = one_over(pair_add(exp2_of(u), both(1.f))), a = pair_mul(z, p);
     *slope = pair_fma(pair_mul(a, pair_fma(p, both(-1.f), both(1.f))), pair_fma(zz, both(3.f * k2 * c), both(k2)), p);
     return a;

@@ -181,6 +181,20 @@ def test_values_that_are_not_finite_reach_the_activation(act, dtype):
     assert int(a.isnan().sum()) == 1 and int(a.isinf().sum()) == 1
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+def test_magnitudes_whose_square_is_infinite(act, dtype):
+    """2^70: the activation is z or 0, the slope 1 or 0 (a power of two is its own code)."""
+    z = torch.tensor([[2.0 ** 70, -2.0 ** 70] * 20], dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    c = binding.ActCheckpoint(40, act=act, fmt="e4m3")
+    a, rec = c.forward(z)
+    dz, again = c.backward(rec, torch.ones_like(z))
+    on = z > 0
+    # all exact, but for GELU in bf16 below -6: its lower tail stays there at -6 Phi(-6) = -6 * 9.866e-10 = -5.92e-9, which 2^-27 = 7.45e-9 holds
+    assert torch.equal(a[on], z[on]) and torch.equal(again, a) and torch.equal(dz, on.to(z.dtype))
+    assert float(a[~on].abs().max()) <= (2.0 ** -27 if act == "gelu" and dtype == "bf16" else 0.0)
+
+
 def test_far_tails_are_finite():
     z = torch.tensor([[-3e4, -200.0, -88.5, -20.0, 0.0, -0.0, 20.0, 88.5, 200.0, 3e4] + [0.0] * 22], device="cuda")
     for act in ("gelu", "gelu_tanh", "silu"):
