@@ -415,8 +415,9 @@ alg_status_t alg_moe_last_status(alg_moe_t h, void *stream, alg_status_t *status
  *              not wanted; the biases' need no biases in the forward pass).  dF needs JOIN, dgate a gate flag, d_post_* POST, d_pre_*
  *              PRE, d_scale JOIN; dF and dgate may be NULL.  Sums run in a fixed order: bitwise repeatable
  *              (which order depends on the types, the sizes and how the rows lie in their 16-byte words).
- * 1 <= D <= ALG_NORM_MAX_D.  Leading dimensions (below 2^30) and addresses may be anything an element may have; D a multiple of 8 with all
- * rows on 16 bytes (vectors too) runs several times faster.  Row b of an output may lie exactly on row b of an operand (Y on R, dR on
+ * 1 <= D <= ALG_NORM_MAX_D.  Leading dimensions (below 2^30) and addresses may be anything an element may have.  Rows on 16 bytes run
+ * fastest; rows that lie off it, but in all matrices alike, take up to twice as long; rows that lie each in its own way, and rows off 16
+ * bytes of more than 8185 columns, several times.  Row b of an output may lie exactly on row b of an operand (Y on R, dR on
  * dY, ...: same address, leading dimension and row length in bytes); any other overlap is ALG_ERR_INVALID_ARG.  M = 0: forward
  * is a no-op, backward writes zero sums.  Workspace (backward): alg_norm_workspace_bytes, 256-byte aligned, no
  * initialisation needed; calls that share one must be ordered on the GPU, others may overlap on any streams.  Forward is one launch,
@@ -464,8 +465,8 @@ alg_status_t alg_norm_last_status(alg_norm_t h, void *stream, alg_status_t *stat
  *                    [act'(G) .* U .* dA | act(G) .* dA]; with A not NULL also the activation once more, for
  *                    the weight gradient of the down projection.
  * One dtype a call: Z, A, dA and dZ are all f32 or all bf16 (arithmetic in fp32, rounded once).  Leading dimensions (below 2^30)
- * and addresses may be anything an element may have; rows on 16 bytes with cols a multiple of 8 run several
- * times faster.  ckpt: 16-byte aligned.  A may be Z and dZ may be dA where both have the same shape and leading dimension;
+ * and addresses may be anything an element may have; rows off 16 bytes or with cols no multiple of 8
+ * take up to three times as long.  ckpt: 16-byte aligned.  A may be Z and dZ may be dA where both have the same shape and leading dimension;
  * any other overlap of outputs with operands is ALG_ERR_INVALID_ARG.  M = 0 is a successful no-op.  One launch a call,
  * no workspace; the calls keep nothing in the handle, so they may overlap on any streams. */
 typedef enum { ALG_Q8_E4M3 = 0, ALG_Q8_INT8 = 1 } alg_q8_t;
