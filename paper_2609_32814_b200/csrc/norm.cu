@@ -135,7 +135,7 @@ cudaError_t launch_norm(const alg_norm_s &h, NormArgs &a, bool alike, bool on16,
   *full = true;
   const int w = eights(BACK, true, a);
   *grid = shape_rows(h, a, w, true, BACK, &smem);
-  const bool exact = on16 && a.D % granule(h) == 0;
+  const bool exact = on16 && a.D % (h.stream_dtype == ALG_F32 && h.dtype == ALG_F32 ? 4 : 8) == 0;   // (copies of an exact row are not rounded up to 16 bytes)
   const int types = (h.stream_dtype == ALG_F32 ? 2 : 0) + (h.dtype == ALG_F32 ? 1 : 0);
   auto *launch = !BACK ? launch_norm_forward_any : w == 1 ? launch_norm_backward_any : launch_norm_backward_any_wide;
   return launch(a, types, alike, exact, *grid, smem, st);

@@ -24,7 +24,7 @@ namespace algproj {
 struct NormArgs;
 // A translation unit each for a direction and type of the residual stream (F, gate and N bf16), and in the backward pass for a norm: the kernels with their form as a constant.
 // types: 2 for an fp32 stream, + 1 for fp32 F, gate and N; alike: see NormArgs::off; exact:
-// rows of whole granules on 16 bytes.
+// rows of whole 16-byte words, on 16 bytes.
 cudaError_t launch_norm_forward_any(NormArgs &a, int types, bool alike, bool exact, int grid, size_t smem, cudaStream_t st);
 cudaError_t launch_norm_backward_any(NormArgs &a, int types, bool alike, bool exact, int grid, size_t smem, cudaStream_t st);   // rows of eight columns a thread
 cudaError_t launch_norm_backward_any_wide(NormArgs &a, int types, bool alike, bool exact, int grid, size_t smem, cudaStream_t st);
@@ -135,7 +135,7 @@ __device__ __forceinline__ void group_sum(float (&v)[K], float4 *red, int &turn,
 // column, whose scalar accesses coalesce.
 // Rows need not begin on a granule (eight bf16 values, four fp32): where all operands lie off it alike, a CTA takes rows that lie off it by the same
 // `shift`, and column c is at c + shift of the granules, so that accesses are whole ones all the same; threads at a row's ends mask theirs.
-// kExact: no shift, and every granule is inside the row or outside; all rows and vectors lie on 16 bytes.  kWhole: and inside, all of them
+// kExact: no shift, and every row is whole 16-byte words of each type; all rows and vectors lie on 16 bytes.  kWhole: and inside, all of them
 // (nothing is asked, which the backward pass has no registers for: gradients of 16384 x 4096 rows 265 us against 311).
 enum { kScalar, kEight, kFours, kExact = 4, kWhole = 8 + kExact };
 template <int HOW>
@@ -653,8 +653,8 @@ cudaError_t launch_rows(NormArgs &a, int grid, size_t smem, cudaStream_t st) {
 template <bool BACK, typename XT, int V, bool LAYER, int FORM>
 cudaError_t launch_form(NormArgs &a, bool on16, int grid, size_t smem, cudaStream_t st) {
   constexpr int kMap = sizeof(XT) == 4 ? kFours : kEight;
-  // forward: rows of whole granules on 16 bytes; backward: such as fill the threads' pieces
-  if (on16 && (BACK ? a.D == a.T * V * 8 : a.D % (kMap == kEight ? 8 : 4) == 0))
+  // forward: rows of whole 16-byte words (of F in bf16: eights) on 16 bytes; backward: such as fill the threads' pieces
+  if (on16 && (BACK ? a.D == a.T * V * 8 : a.D % 8 == 0))
     return launch_rows<BACK, XT, __nv_bfloat16, kMap | (BACK ? kWhole : kExact), V, LAYER, FORM>(a, grid, smem, st);
   return launch_rows<BACK, XT, __nv_bfloat16, kMap, V, LAYER, FORM>(a, grid, smem, st);
 }

@@ -205,6 +205,18 @@ def test_many_rows(kind, dtype, stream, m, d):
     b.check_backward(y, b.h.backward(y, dY=b.dY, dN=b.dN, **b.call()))
 
 
+@pytest.mark.parametrize("dtype,stream", [("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("kind,vectors", [("rms", False), ("layer", True)])
+@pytest.mark.parametrize("m,d,pitch", [(1, 596, 0), (1, 2956, 0), (7, 596, 600), (3, 4, 8), (5, 8188, 8192)])
+def test_rows_on_sixteen_bytes_that_end_inside_them(dtype, stream, kind, vectors, m, d, pitch):
+    """Four columns are 16 bytes of fp32 and half of that in bf16: the rows begin on 16 bytes and end between them."""
+    b = Border(m, d, kind, True, True, "element", True, vectors, dtype, stream, pitch=pitch)
+    y, n = b.h.forward(b.R, **b.call())
+    b.check_forward(y, n)
+    b.check_backward(y, b.h.backward(y, dY=b.dY, dN=b.dN, **b.call()))
+    assert b.h.last_status() == 0
+
+
 @pytest.mark.parametrize("kind,back", [("rms", 0), ("layer", 0), ("rms", 1), ("layer", 1)])
 def test_operands_that_lie_off_sixteen_bytes_each_in_its_own_way(kind, back):
     """Rows of R, F and the outputs begin at different places of a 16-byte word: single accesses, and the same results."""
