@@ -464,7 +464,9 @@ alg_status_t alg_norm_last_status(alg_norm_t h, void *stream, alg_status_t *stat
  *   act_backward     from the records of Z (as they read back) and dA (M x cols): dZ = act'(Z) .* dA, or
  *                    [act'(G) .* U .* dA | act(G) .* dA]; with A not NULL also the activation once more, for
  *                    the weight gradient of the down projection.
- * One dtype a call: Z, A, dA and dZ are all f32 or all bf16 (arithmetic in fp32, rounded once).  Leading dimensions (below 2^30)
+ * One dtype a call: Z, A, dA and dZ are all f32 or all bf16 (arithmetic in fp32, rounded once; exponentials and reciprocals are the
+ * GPU's approximate ones, off by a few units, and |z| or z^2 units where |z| is large.  GELU_ERF: the normal distribution's tail is a fit that
+ * keeps its bits however small it is, to 8e-4 of itself for bf16, a fifth of half a step, to 8 units of 2^-24 for fp32).  Leading dimensions (below 2^30)
  * and addresses may be anything an element may have; rows off 16 bytes or with cols no multiple of 8
  * take up to three times as long.  ckpt: 16-byte aligned.  A may be Z and dZ may be dA where both have the same shape and leading dimension;
  * any other overlap of outputs with operands is ALG_ERR_INVALID_ARG.  M = 0 is a successful no-op.  One launch a call,

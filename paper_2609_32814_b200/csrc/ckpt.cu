@@ -7,7 +7,7 @@
 //
 // One pass over memory either way, eight columns (16 bytes of bf16) a thread: four neighbouring threads are a block and
 // find its maximum by two shuffles.  Bound by HBM: 16384 x 7168 fp32 stored and loaded 180 us (6.57 TB/s), SwiGLU 16384 x 6144 both
-// passes 295 us (6.18), GELU 8003 x 4096 68 us (5.84; with erff and one value an instruction 113, bound by the arithmetic).
+// passes 290 us (6.28), GELU 8003 x 4096 71 us (5.54; with erff and one value an instruction 113, bound by the arithmetic), in fp32 115 (6.3).
 #include <cuda_fp8.h>
 
 #include <new>
@@ -121,6 +121,36 @@ __device__ __forceinline__ uint64_t one_over(uint64_t x) {
   return pair(lo, hi);
 }
 
+// Phi(n), the normal distribution's lower tail, for n <= 0, and e = exp(-n^2 / 2).  However small it is, the tail keeps its bits.
+// bf16 results: 2^q(n), q of degree eight fitted to log2 Phi(n) on [-13.3, 0] (beyond, the tail is 0 in fp32): 8.1e-4 of the value at most, a fifth of half a
+// step, and 5.6e-7 at most.
+// fp32: Phi(n) / e falls smoothly from 1/2 towards 0.4 / |n|: it is t P(t) with t = 1 / (1 - 0.275 n) and P of degree eight, fitted to 3.9e-8 of its value, 8
+// units of 2^-24 with its own roundings; what grows is the rounding of n^2, n^2 units.  (For bf16 that took 74 us of both passes over 8003 x 4096, where 2^q takes 71.)
+template <typename T>
+__device__ __forceinline__ uint64_t normal_tail(uint64_t n, uint64_t e) {
+  uint64_t p;
+  if (sizeof(T) == 2) {
+    p = pair_fma(n, both(4.11549252e-08f), both(2.46185356e-06f));
+    p = pair_fma(p, n, both(6.28251626e-05f));
+    p = pair_fma(p, n, both(9.06560959e-04f));
+    p = pair_fma(p, n, both(8.35534306e-03f));
+    p = pair_fma(p, n, both(5.36305293e-02f));
+    p = pair_fma(p, n, both(-4.58744711e-01f));
+    p = pair_fma(p, n, both(1.1511728f));
+    return exp2_of(pair_fma(p, n, both(-0.999998488f)));
+  }
+  const uint64_t t = one_over(pair_fma(n, both(-0.275f), both(1.f)));
+  p = pair_fma(t, both(0.0262493369f), both(-0.106020485f));
+  p = pair_fma(p, t, both(0.120182197f));
+  p = pair_fma(p, t, both(-0.0233438075f));
+  p = pair_fma(p, t, both(0.0796022513f));
+  p = pair_fma(p, t, both(0.0826022953f));
+  p = pair_fma(p, t, both(0.10123601f));
+  p = pair_fma(p, t, both(0.109789479f));
+  p = pair_fma(p, t, both(0.109702743f));
+  return pair_mul(pair_mul(p, t), e);
+}
+
 // act(z) of two values, and its derivative.  (Two at a time and packed at once: eight would hold 56 registers where 40 do, and threads
 // are what keeps the memory busy.)
 template <typename T, int ACT>
@@ -144,31 +174,19 @@ __device__ __forceinline__ uint64_t act2(uint64_t z, uint64_t *slope) {
   if (ACT == ALG_ACT_GELU_ERF) {
     float lo, hi;
     halves(z, lo, hi);
-    const uint64_t zphi = pair_mul(pair_mul(z, both(0.39894228040143268f)), exp2_of(pair_mul(pair_mul(z, z), both(-0.5f * log2e))));
-    if (sizeof(T) == 4) {
-      const uint64_t p = pair(fmaf(0.5f, erff(lo * 0.70710678118654752f), 0.5f), fmaf(0.5f, erff(hi * 0.70710678118654752f), 0.5f));
-      *slope = pair_add(zphi, p);
-      return pair_mul(z, p);
-    }
-    // bf16 results: the lower tail 2^p(|z|) of the projection kernels' epilogues, off by 2.4e-6 at most
-    const uint64_t u = pair(fminf(fabsf(lo), 6.f), fminf(fabsf(hi), 6.f));
-    uint64_t q = pair_fma(u, both(3.3093889e-05f), both(-7.6922908e-04f));
-    q = pair_fma(q, u, both(8.0807470e-03f));
-    q = pair_fma(q, u, both(-5.3412151e-02f));
-    q = pair_fma(q, u, both(-4.5877093e-01f));
-    q = pair_fma(q, u, both(-1.1512017f));
-    q = pair_fma(q, u, both(-0.99999309f));
-    const uint64_t tail = exp2_of(q);
-    // z - u tail above 0, -u tail below: u for |z| is off by less than the tail there, and an infinite z stays what it is
+    const uint64_t n = pair(fmaxf(-fabsf(lo), -13.3f), fmaxf(-fabsf(hi), -13.3f));   // (whose tail is 0, as that of an infinity should be)
+    const uint64_t e = exp2_of(pair_mul(pair_mul(n, n), both(-0.5f * log2e))), tail = normal_tail<T>(n, e);
+    // Phi(z) is the tail or 1 - tail, never a difference of two halves: that would leave nothing of it from -5.5 on
+    float t0, t1, h0, h1;
+    halves(tail, t0, t1);
+    halves(pair_fma(tail, both(-1.f), both(1.f)), h0, h1);
+    *slope = pair_fma(pair_mul(z, both(0.39894228040143268f)), e, pair(lo < 0.f ? t0 : h0, hi < 0.f ? t1 : h1));
     auto above = [](float v) {   // max(v, 0), NaN for NaN
       float r;
       asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(v));
       return r;
     };
-    float h0, h1;
-    halves(pair_fma(tail, both(-1.f), both(0.5f)), h0, h1);
-    *slope = pair_add(zphi, pair_add(pair(copysignf(h0, lo), copysignf(h1, hi)), both(0.5f)));
-    return pair_fma(pair_mul(u, both(-1.f)), tail, pair(above(lo), above(hi)));
+    return pair_fma(n, tail, pair(above(lo), above(hi)));   // z - |z| tail above 0, -|z| tail below
   }
   *slope = both(1.f);
   return z;

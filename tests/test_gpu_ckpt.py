@@ -268,3 +268,27 @@ def test_refusals_leave_the_outputs_alone():
     assert binding.launch_count() == before
     c.forward(wide[:, :64], out=wide[:, 64:128])                       # column slices of one buffer do not overlap
     assert binding.launch_count() == before + 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lower_tail_of_gelu_keeps_its_bits(dtype):
+    """z Phi(z) and its slope down to -13, where Phi is 6e-39, to a bound that shrinks with them.
+
+    fp32, in units of 2^-24 of the value: Phi(-u) = t P(t) exp(-u^2/2), t = 1 / (1 + 0.275 u): fit and evaluation 8, t off by 3 (a rounding and an
+    approximate reciprocal of one unit in the last place) times 2.9 at most (the logarithmic slope of t P(t)), exp2 of two units in the last place 4, its argument
+    0.72 u^2 off by three roundings: 3 u^2 / 2; products and sums 6.  Together less than 32 + 2 z^2, of Phi(z) + |z| phi(z) for the slope.  bf16: a fit to
+    8.1e-4 of the value, 13 600 units (its exponent's own roundings among them), which is a fifth of half a step."""
+    z = (torch.arange(-104, 104, dtype=torch.float64) / 8).view(-1, 16).repeat(1, 2)[:, :32].contiguous()     # int8 codes under a scale of 1/8
+    z[:, 0] = z[:, 0].abs()
+    z[:, 31] = 13.0                                                                                            # (every block has that scale)
+    c = binding.ActCheckpoint(32, act="gelu", fmt="int8")
+    a, rec = c.forward(z.to(DT[dtype]).cuda())
+    assert torch.equal(c.load(rec, out_dtype=torch.float32).double().cpu(), z)
+    dz, again = c.backward(rec, torch.ones_like(a))
+    # (special.ndtr is a difference below -1, and 0 from -8.4 on)
+    Phi, zphi = torch.erfc(-z * math.sqrt(0.5)) / 2, z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    rel = (32 + (13600 if dtype == "bf16" else 0) + 2 * z * z) * 2.0 ** -24
+    half, least = torch.finfo(DT[dtype]).eps / 2, 16 * 2.0 ** -126
+    for got, want, size in ((a, z * Phi, (z * Phi).abs()), (again, z * Phi, (z * Phi).abs()), (dz, Phi + zphi, Phi + zphi.abs())):
+        off = (got.double().cpu() - want).abs() / (rel * size + half * want.abs() + least)
+        assert float(off.max()) <= 1.0, (float(off.max()), float(z.flatten()[off.argmax()]))
