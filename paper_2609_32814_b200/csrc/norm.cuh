@@ -12,7 +12,7 @@
 // A thread keeps the sums of its columns over all rows of its group in registers, the groups of a CTA meet in shared memory at the end, and
 // a second launch adds the CTAs' sums in CTA order.
 // Measured, back to back: forward, 32768 x 4096 bf16, RMS, gate of each element 205 to 210 us (6.4 TB/s); backward, LayerNorm, 16384 x 4096, fp32
-// stream, gate of each element 271 us (5.4 TB/s: the sums leave eight columns a thread, three exchanges a row); one row 4 us.
+// stream, gate of each element 285 us (5.2 TB/s: the sums leave eight columns a thread, three exchanges a row); one row 4 us.
 #pragma once
 
 #include "common.cuh"
@@ -523,7 +523,11 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
     const float rx = rsqrtf(s[0] * inv_d + a.eps), rf = post ? rsqrtf(s[1] * inv_d + a.eps) : 1.f;
     const float mhv = s[2] * inv_d * rx;
     // the row's gate and its slope
-    const float gr = gate_row && sig ? sigmoid(gate_1) : gate_1, gs = sig ? gr * (1.f - gr) : 1.f;
+    float gr = gate_1, gs = 1.f;
+    if (gate_row && sig) {
+      float e1;
+      gr = sigmoid(gate_1, e1), gs = gr * (gr * e1);
+    }
     F8 e[V];   // gradient of V
     float m[3] = {0.f, 0.f, 0.f};
 #pragma unroll
@@ -541,33 +545,35 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const NormAr
       if (!join) continue;
       const F8 f = fc_of(v) * rf, w = vector8<MAP, V, FORM>(a, vec, kVecW, cols, v);
       F8 dg = d[v] * gr;   // the gradient behind the gate
-      F8 slope;
+      auto of_gate = [&] {
+        F8 b = f * w;
+        if (FULL) b = b + vector8<MAP, V, FORM>(a, vec, kVecB, cols, v);
+        return b * d[v];
+      };
       if (gate_el) {
         F8 z = V == 1 ? q[v] : cols.load(staged<BT, MAP>(a, st, kG, row, shift), v);
-        if (sig) {
-          float p[8];
-          to8(z, p);
+        if (sig) {   // the gate's gradient pair by pair: with the slopes kept for later the narrow LayerNorm spills (16384 x 4096: 330 us, so 285)
+          F8 b, add;
+          if (FULL) add = vector8<MAP, V, FORM>(a, vec, kVecB, cols, v);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] = sigmoid(p[j]);
-          z = from8(p);
-          slope = fma8(z * z, -1.f, z);
+          for (int j = 0; j < 4; ++j) {
+            float lo, hi, e0, e1;
+            halves(z.p[j], lo, hi);
+            lo = sigmoid(lo, e0), hi = sigmoid(hi, e1);
+            z.p[j] = pair(lo, hi);
+            b.p[j] = pair_mul(f.p[j], w.p[j]);
+            if (FULL) b.p[j] = pair_add(b.p[j], add.p[j]);
+            b.p[j] = pair_mul(pair_mul(b.p[j], d[v].p[j]), pair_mul(z.p[j], pair_mul(z.p[j], pair(e0, e1))));
+          }
+          if (to_gate) cols.store((BT *)(a.dg + (uint64_t)row * a.pitch_dg) - shift, v, b);
         }
         dg = d[v] * z;
       }
       sum[2][v] = fma8(dg, f, sum[2][v]);
       if (FULL) sum[3][v] = sum[3][v] + dg;
       e[v] = dg * w;
-      if (gate_row || (gate_el && to_gate)) {
-        F8 b = f * w;
-        if (FULL) b = b + vector8<MAP, V, FORM>(a, vec, kVecB, cols, v);
-        b = b * d[v];
-        if (gate_el) {
-          if (sig) b = b * slope;
-          cols.store((BT *)(a.dg + (uint64_t)row * a.pitch_dg) - shift, v, b);
-        } else {
-          m[2] += sum8(b);
-        }
-      }
+      if (gate_row) m[2] += sum8(of_gate());
+      else if (gate_el && to_gate && !sig) cols.store((BT *)(a.dg + (uint64_t)row * a.pitch_dg) - shift, v, of_gate());
       if (post) {
         if (layer) m[0] += sum8(e[v]);
         m[1] += dot8(e[v], f);

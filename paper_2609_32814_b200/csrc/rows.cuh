@@ -129,10 +129,19 @@ __device__ __forceinline__ float dot8(const F8 &a, const F8 &b) {
   halves(pair_add(pair_fma(a.p[0], b.p[0], pair_mul(a.p[1], b.p[1])), pair_fma(a.p[2], b.p[2], pair_mul(a.p[3], b.p[3]))), lo, hi);
   return lo + hi;
 }
-// 1 / (1 + exp(-x)), within 4 units: two approximations of the special function unit.
+// 1 / (1 + exp(-x)), by two approximations of the special function unit: off by 7 units of 2^-24, and below 0 by 2 |x| more from the rounding of x log2 e.
 __device__ __forceinline__ float sigmoid(float x) {
   float e, r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+// The same, and what makes its slope a product, s (s e): s (1 - s) loses its bits as s nears 1 (0.9 % at x = 12, all from 17 on).
+// (Below -88.4, where s is 0 already, e would become infinite.)
+__device__ __forceinline__ float sigmoid(float x, float &e) {
+  float r;
+  asm("max.NaN.f32 %0, %1, 0fC2B0CCCD;" : "=f"(r) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(r * -1.4426950408889634f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }

@@ -389,3 +389,48 @@ def test_refusals():
     with pytest.raises(binding.AlgError) as e:
         binding.BlockNorm(8193)
     assert e.value.code == 2
+
+
+@pytest.mark.parametrize("kind,gate,dtype,stream,d", [("rms", "element", "bf16", "bf16", 512), ("layer", "element", "bf16", "f32", 264), ("rms", "row", "bf16", "bf16", 512),
+                                                      ("layer", "row", "f32", "f32", 96), ("rms", "element", "f32", "f32", 333), ("layer", "element", "bf16", "bf16", 4104)])
+def test_slope_of_a_saturated_sigmoid(kind, gate, dtype, stream, d):
+    """The gate's gradient where the sigmoid is nearly 0 or 1, to a bound that shrinks with the slope.
+
+    slope = s s e with e = exp(-x), s = 1 / (1 + e): in units of 2^-24 of it e is off by 4 + 2 |x| (exp2 of two units in the last place, the
+    rounding of x log2 e and of the constant), which reaches the slope at most once (its logarithmic derivative in e is (1 - e) / (1 + e)), the
+    reciprocal and its sum by 3 each time, two products by 2: 12 + 2 |x| <= 52 for |x| <= 20, beside the 64 of the module's account."""
+    m = 16
+    b = Border(m, d, kind, True, True, gate, True, True, dtype, stream)
+    x = torch.tensor([8.0, -8.0, 12.0, -12.0, 16.0, -16.0, 20.0, -20.0], dtype=torch.float64)
+    b.gate.copy_(x.repeat(2) if gate == "row" else x.repeat(-(-d // 8))[:d].expand(m, d))
+    b.w["gate"] = b.gate.double().cpu()
+    y, n = b.h.forward(b.R, **b.call())
+    b.check_forward(y, n)
+    got = b.h.backward(y, dY=b.dY, dN=b.dN, **b.call())
+    b.check_backward(y, got)
+    w, y64 = b.w, y.double().cpu()
+    yl = y64.clone().requires_grad_(True)
+    T = w["dY"] + torch.autograd.grad(norm(yl, kind, w["pre_weight"], w["pre_bias"]), yl, w["dN"])[0]
+    size = w["dY"].abs() + through(y64, kind, w["dN"] * w["pre_weight"])
+    s = 1 / (1 + torch.exp(-w["gate"].abs()))
+    slope = torch.exp(-w["gate"].abs()) * s * s
+    f = b.factor(dict(w, gate=None))
+    want, bound = T * f * b.branch(w), size * f.abs() * norm_size(w["F"], kind, w["post_weight"], w["post_bias"])
+    if gate == "row":
+        want, bound = want.sum(1), bound.sum(1)
+    near(got["gate"], want * slope, bound * slope, "dgate", 2 * U)
+
+
+@pytest.mark.parametrize("gate", ["row", "element"])
+def test_gates_that_shut_a_row_off(gate):
+    """A sigmoid of -infinity, of the types' lowest values and of +infinity: the gate is 0 or 1 and has no slope."""
+    for dtype in ("bf16", "f32"):
+        b = Border(6, 72, "rms", True, True, gate, True, True, dtype, "f32")
+        low = torch.finfo(DT[dtype]).min
+        x = torch.tensor([-math.inf, low, -1000.0, math.inf, -low, 1000.0], dtype=torch.float64)
+        b.gate.copy_(x if gate == "row" else x[:, None].expand(6, 72))
+        y, n = b.h.forward(b.R, **b.call())
+        assert torch.equal(y[:3], b.R[:3])
+        got = b.h.backward(y, dY=b.dY, dN=b.dN, **b.call())
+        assert all(bool(torch.isfinite(v).all()) for v in got.values())
+        assert bool((got["gate"] == 0).all()) and bool((got["F"][:3] == 0).all()) and bool((got["F"][3:] != 0).any(1).all())
