@@ -433,6 +433,8 @@ typedef enum { ALG_NORM_RMS = 0, ALG_NORM_LAYER = 1 } alg_norm_kind_t;
 alg_status_t alg_norm_create(alg_norm_t *out, int D, alg_norm_kind_t kind, int flags, float eps, alg_dtype_t stream_dtype,
                              alg_dtype_t dtype);
 alg_status_t alg_norm_destroy(alg_norm_t h);
+/* WAIT_LIMIT_CYCLES and TEST_STALL_BYTES (at most 65536; of a row's copies) alone. */
+alg_status_t alg_norm_set_option(alg_norm_t h, alg_option_t option, int64_t value);
 alg_status_t alg_norm_workspace_bytes(alg_norm_t h, size_t *bytes);
 alg_status_t alg_norm_forward(alg_norm_t h, const void *R, int64_t ldr, const void *F, int64_t ldf, const void *gate, int64_t ldg,
                               const float *post_weight, const float *post_bias, const float *scale, float alpha,

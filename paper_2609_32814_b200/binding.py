@@ -44,7 +44,7 @@ EXPORTS = [
     "alg_ffn_gated_create", "alg_ffn_gated_forward", "alg_proj_grad_create", "alg_proj_grad_destroy",
     "alg_proj_grad_workspace_bytes", "alg_proj_grad_input", "alg_proj_grad_weight", "alg_proj_grad_last_status", "alg_ffn_macs", "alg_ffn_last_status", "alg_ffn_set_timing", "alg_ffn_get_timing", "alg_status_string", "alg_launch_count",
     "alg_moe_create", "alg_moe_destroy", "alg_moe_workspace_bytes", "alg_moe_forward", "alg_moe_last_status",
-    "alg_norm_create", "alg_norm_destroy", "alg_norm_workspace_bytes", "alg_norm_forward", "alg_norm_backward", "alg_norm_last_status",
+    "alg_norm_create", "alg_norm_destroy", "alg_norm_set_option", "alg_norm_workspace_bytes", "alg_norm_forward", "alg_norm_backward", "alg_norm_last_status",
     "alg_ckpt_create", "alg_ckpt_destroy", "alg_ckpt_row_bytes", "alg_ckpt_store", "alg_ckpt_load", "alg_ckpt_act_forward",
     "alg_ckpt_act_backward",
 ]
@@ -108,6 +108,7 @@ def lib() -> ctypes.CDLL:
         L.alg_moe_last_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         L.alg_norm_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, ctypes.c_float, i32, i32]
         L.alg_norm_destroy.argtypes = [vp]
+        L.alg_norm_set_option.argtypes = [vp, i32, i64]
         L.alg_norm_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
         L.alg_norm_forward.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, ctypes.c_float, vp, vp, i64, vp, i64, vp, i64, vp]
         L.alg_norm_backward.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, ctypes.c_float, vp, i64, vp, i64, vp, i64,
@@ -525,6 +526,7 @@ class BlockNorm(_Handle):
     ``join``: F is added to the residual stream R (else Y is R); ``post``: F is normed; ``pre``: N is wanted; ``gate``: None, "row"
     (one value for each row) or "element".  R, Y and their gradients have ``stream_dtype``, F, gate, N and theirs ``dtype``."""
     _destroy = "alg_norm_destroy"
+    _set_option = "alg_norm_set_option"
 
     def __init__(self, D, kind="rms", join=False, pre=True, post=False, gate=None, gate_act=None, eps=1e-6, dtype="bf16", stream_dtype="bf16"):
         super().__init__()
@@ -541,9 +543,6 @@ class BlockNorm(_Handle):
         out = ctypes.c_size_t()
         _check(lib().alg_norm_workspace_bytes(self._h, ctypes.byref(out)), "alg_norm_workspace_bytes")
         self._bytes = out.value
-
-    def set_option(self, name, value):
-        raise NotImplementedError("norm handles have no options")
 
     def workspace_bytes(self) -> int:
         """Bytes a backward call with column sums needs."""

@@ -13,6 +13,8 @@ struct alg_norm_s {
   alg_dtype_t stream_dtype = ALG_BF16, dtype = ALG_BF16;
   int device = 0, num_sms = 148;
   int *d_status = nullptr;
+  long long wait_limit = kDefaultWaitLimit;
+  uint32_t stall = 0;
 };
 
 namespace algproj {
@@ -211,6 +213,10 @@ alg_status_t alg_norm_destroy(alg_norm_t h) {
   return ALG_OK;
 }
 
+alg_status_t alg_norm_set_option(alg_norm_t h, alg_option_t option, int64_t value) {
+  return h ? wait_option(&h->wait_limit, &h->stall, option, value) : ALG_ERR_INVALID_ARG;
+}
+
 alg_status_t alg_norm_workspace_bytes(alg_norm_t h, size_t *bytes) {
   if (!h || !bytes) return ALG_ERR_INVALID_ARG;
   *bytes = (sums_bytes(*h) + 255) / 256 * 256;
@@ -252,7 +258,7 @@ alg_status_t alg_norm_forward(alg_norm_t h, const void *R, int64_t ldr, const vo
   a.gate = row ? gate : nullptr;
   a.post_w = post_weight, a.post_b = post_bias, a.scale = scale, a.pre_w = pre_weight, a.pre_b = pre_bias;
   a.y = (uint8_t *)Y, a.pitch_y = (uint32_t)(ldy * ex), a.out = (uint8_t *)N, a.pitch_out = (uint32_t)(ldn * eb);
-  a.status = h->d_status, a.wait_limit = kDefaultWaitLimit;
+  a.status = h->d_status, a.wait_limit = h->wait_limit, a.stall = h->stall;
   Granules gr = {granule(*h)};
   gr.add(R, ldr, ex, M), gr.add(F, ldf, eb, M), gr.add(el ? gate : nullptr, ldg, eb, M), gr.add(Y, ldy, ex, M), gr.add(N, ldn, eb, M);
   gr.tell(a);
@@ -335,7 +341,7 @@ alg_status_t alg_norm_backward(alg_norm_t h, const void *Y, int64_t ldy, const v
   a.M = (uint32_t)M, a.D = D, a.flags = h->flags, a.layer = h->kind == ALG_NORM_LAYER, a.eps = h->eps, a.alpha = alpha;
   a.post_w = post_weight, a.post_b = post_bias, a.scale = scale, a.pre_w = pre_weight;
   a.part = sums ? (float *)workspace : nullptr;
-  a.status = h->d_status, a.wait_limit = kDefaultWaitLimit;
+  a.status = h->d_status, a.wait_limit = h->wait_limit, a.stall = h->stall;
   int grid = 0;
   bool full = d_post_bias || d_pre_bias;
   if (M > 0 && launch_norm<true>(*h, a, gr.alike, on16 && gr.on16, &full, &grid, st) != cudaSuccess) return ALG_ERR_CUDA;

@@ -65,6 +65,7 @@ struct NormArgs {
   float *part;                  // [CTAs][kSums][D]
   int *status;
   long long wait_limit;
+  uint32_t stall;               // test aid: bytes that are expected of a row beside its own, and never come
 };
 
 // The form of a call: what it does, as a constant of a kernel (kAny: found out at run time, with every branch that costs: gradients of
@@ -286,7 +287,7 @@ __device__ __forceinline__ void issue_row(const NormArgs &a, uint32_t stage, uin
   auto from = [&](int k) { return a.op[k] + (uint64_t)row * a.pitch[k]; };
   auto bytes = [&](int k) { return OFF ? (((uint32_t)(uintptr_t)from(k) & 15u) + a.bytes[k] + 15u) & ~15u : a.bytes[k]; };
   if (t == 0) {
-    uint32_t total = 0;
+    uint32_t total = a.stall;
 #pragma unroll
     for (int k = 0; k < kOps; ++k) total += a.op[k] ? bytes(k) : 0u;
     tc::mbar_expect_tx(bar, total);
@@ -308,7 +309,8 @@ __device__ __forceinline__ uint32_t row_step(const NormArgs &a) { return gridDim
 __device__ __forceinline__ uint32_t first_row(const NormArgs &a, int g) { return blockIdx.x % a.period + a.period * (blockIdx.x / a.period * a.G + g); }
 
 // The loop over a group's rows: body(row, stage, release); release() once the row's operands are read and a barrier of the group has
-// followed.
+// followed.  A wait that runs out says so in the status word.  From then on nothing is right and nothing more is asked for, but every thread still goes
+// the same way to the end, where it gives the copies on their way time to land: the CTA's shared memory is not handed on before.
 template <int MAP, int V, typename XT, typename BT, typename Body>
 __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vectors *vec, Body body) {
   const int g = threadIdx.x / a.T, t = threadIdx.x - g * a.T;
@@ -328,7 +330,7 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
   __syncthreads();
   int s = 0;
   uint32_t parity = 0;
-  bool failed = false;   // after a wait that ran out nothing is right, but every thread still goes the same way to the end
+  bool failed = false;
   for (uint32_t row = first; row < a.M; row += step) {
     if (!tc::mbar_try_wait(bar + 8 * s, parity) && !failed) {
       const long long t0 = clock64();
@@ -340,10 +342,13 @@ __device__ __forceinline__ void each_row(const NormArgs &a, uint8_t *smem, Vecto
         }
     }
     body(row, (const uint8_t *)rows + s * a.stage_bytes, [&] {
-      if (row + a.stages * step < a.M) issue_row<!(MAP & kExact)>(a, rows_at + s * a.stage_bytes, bar + 8 * s, row + a.stages * step, t);
+      if (!failed && row + a.stages * step < a.M) issue_row<!(MAP & kExact)>(a, rows_at + s * a.stage_bytes, bar + 8 * s, row + a.stages * step, t);
     });
     if (++s == a.stages) s = 0, parity ^= 1;
   }
+  if (failed)
+    for (const long long t0 = clock64(); clock64() - t0 < kLandCycles;) {
+    }
 }
 
 // The gate of a row, asked for one row ahead.

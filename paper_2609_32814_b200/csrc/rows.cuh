@@ -146,6 +146,8 @@ __device__ __forceinline__ float sigmoid(float x, float &e) {
   return r;
 }
 
+constexpr long long kLandCycles = 2000000;   // about a millisecond, in which any copy lands
+constexpr int kMaxStall = 1 << 16;             // of ALG_OPT_TEST_STALL_BYTES: what a barrier counts stays below 2^20
 constexpr int64_t kMaxLd = 1 << 30;   // (the kernels count the bytes between rows in 32 bits)
 inline size_t elem_size(alg_dtype_t t) { return t == ALG_BF16 ? 2 : 4; }
 inline bool on_16(const void *p, int64_t ld, size_t elem) { return ((uintptr_t)p & 15u) == 0 && ((size_t)ld * elem) % 16 == 0; }
@@ -170,6 +172,14 @@ inline bool meet(const RowSpan &a, const RowSpan &b) {
   return d < lo.width || d + hi.width > a.pitch;
 }
 inline bool same_rows(const RowSpan &a, const RowSpan &b) { return a.at == b.at && a.pitch == b.pitch && a.width == b.width; }
+
+// The options of handles whose only ones are about their waits.
+inline alg_status_t wait_option(long long *limit, uint32_t *stall, alg_option_t option, int64_t value) {
+  if (option == ALG_OPT_WAIT_LIMIT_CYCLES && value >= 1000) *limit = value;
+  else if (option == ALG_OPT_TEST_STALL_BYTES && value >= 0 && value <= kMaxStall && value % 16 == 0) *stall = (uint32_t)value;
+  else return ALG_ERR_INVALID_ARG;
+  return ALG_OK;
+}
 
 // The current device, which has to be the one a handle was made on, and of the kind the kernels are built for.
 inline alg_status_t kernel_device(int *dev, int *num_sms) {

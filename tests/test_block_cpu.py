@@ -58,3 +58,8 @@ def test_expert_handles_refuse_bad_arguments_first():
     assert L.alg_moe_workspace_bytes(None, 1, ctypes.byref(n)) == 1 and L.alg_moe_destroy(None) == 1
     assert L.alg_moe_forward(None, None, 0, 1, None, None, None, None, None, 0, 1, None, None, None, 0, None) == 1
     assert L.alg_moe_last_status(None, None, ctypes.byref(s)) == 1
+
+
+def test_norm_handles_have_options():
+    L = _lib()
+    assert L.alg_norm_set_option(None, 5, 1000) == 1

@@ -434,3 +434,40 @@ def test_gates_that_shut_a_row_off(gate):
         got = b.h.backward(y, dY=b.dY, dN=b.dN, **b.call())
         assert all(bool(torch.isfinite(v).all()) for v in got.values())
         assert bool((got["gate"] == 0).all()) and bool((got["F"][:3] == 0).all()) and bool((got["F"][3:] != 0).any(1).all())
+
+
+@pytest.mark.parametrize("kind,dtype,stream,m,d,pitch", [("rms", "bf16", "bf16", 5000, 64, 0), ("layer", "bf16", "f32", 900, 1024, 0), ("layer", "f32", "f32", 310, 8192, 0),
+                                                         ("rms", "bf16", "bf16", 700, 1001, 1003)])
+def test_a_wait_that_runs_out_ends_the_call(kind, dtype, stream, m, d, pitch):
+    """Copies that never come (the rows' barriers are told to expect more bytes than are sent; every copy that is sent lands): the calls return, the status
+    word says so and is cleared by reading it, nothing beside the outputs is touched, and the next calls are right, bit for bit."""
+    b = Border(m, d, kind, True, True, "element", True, True, dtype, stream, pitch=pitch)
+    kw = dict(b.call())
+    y, n = b.h.forward(b.R, **kw, out=b.out["Y"], normed=b.out["N"])
+    y = y.clone()
+    first = {"Y": y, "N": n.clone(), **{k: v.clone() for k, v in b.h.backward(y, dY=b.dY, dN=b.dN, **kw).items()}}
+    b.h.set_option("test_stall_bytes", 1024)
+    for limit in (1000, 20000, 4_000_000):
+        b.h.set_option("wait_limit_cycles", limit)
+        b.h.forward(b.R, **kw, out=b.out["Y"], normed=b.out["N"])
+        assert b.h.last_status() == 6 and b.h.last_status() == 0
+        b.h.backward(y, dY=b.dY, dN=b.dN, **kw)
+        assert b.h.last_status() == 6 and b.h.last_status() == 0
+    b.h.set_option("test_stall_bytes", 0)
+    b.h.set_option("wait_limit_cycles", 4_000_000_000)
+    y2, n2 = b.h.forward(b.R, **kw, out=b.out["Y"], normed=b.out["N"])
+    again = {"Y": y2, "N": n2, **b.h.backward(y, dY=b.dY, dN=b.dN, **kw)}
+    assert b.h.last_status() == 0
+    for k in first:
+        assert torch.equal(first[k], again[k]), k
+    if pitch:
+        for t in (b.R, b.F, b.out["Y"], b.out["N"]):
+            assert bool((t._base[:m * pitch].view(m, pitch)[:, d:] == 5.0).all())
+    with pytest.raises(binding.AlgError):
+        b.h.set_option("test_stall_bytes", 8)
+    with pytest.raises(binding.AlgError):
+        b.h.set_option("test_stall_bytes", 65552)
+    with pytest.raises(binding.AlgError):
+        b.h.set_option("wait_limit_cycles", 999)
+    with pytest.raises(binding.AlgError):
+        b.h.set_option("stage_k", 64)
