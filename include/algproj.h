@@ -389,11 +389,14 @@ typedef enum { ALG_MOE_SOFTMAX = 0, ALG_MOE_SIGMOID = 1 } alg_moe_score_t;
 alg_status_t alg_moe_create(alg_moe_t *out, int D, int F, int E, int top_k, alg_moe_score_t score, int renormalise, float route_scale,
                             alg_dtype_t router_dtype);
 alg_status_t alg_moe_destroy(alg_moe_t h);
+/* WAIT_LIMIT_CYCLES and TEST_STALL_BYTES (at most 65536; of the rows' copies) alone. */
+alg_status_t alg_moe_set_option(alg_moe_t h, alg_option_t option, int64_t value);
 alg_status_t alg_moe_workspace_bytes(alg_moe_t h, int64_t max_M, size_t *bytes);
 alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M, const void *W_router, const float *select_bias,
                              const void *W_gate_up, const void *W_down, void *Y, int64_t ldy, alg_dtype_t y_dtype, int32_t *experts,
                              float *weights, void *workspace, size_t workspace_bytes, void *stream);
-/* Reads and clears the handle's device status word, as alg_proj_last_status. */
+/* Reads and clears the handle's device status word, as alg_proj_last_status; after ALG_ERR_DEVICE_TIMEOUT also the counters, without which
+ * the handle's later calls would not be right. */
 alg_status_t alg_moe_last_status(alg_moe_t h, void *stream, alg_status_t *status);
 
 /* ---- a block's border: norms before and after a block, with its gate and residual scale ----------------

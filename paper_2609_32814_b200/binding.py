@@ -43,7 +43,7 @@ EXPORTS = [
     "alg_ffn_workspace_bytes", "alg_ffn_forward", "alg_ffn_host_workspace_bytes", "alg_ffn_forward_host",
     "alg_ffn_gated_create", "alg_ffn_gated_forward", "alg_proj_grad_create", "alg_proj_grad_destroy",
     "alg_proj_grad_workspace_bytes", "alg_proj_grad_input", "alg_proj_grad_weight", "alg_proj_grad_last_status", "alg_ffn_macs", "alg_ffn_last_status", "alg_ffn_set_timing", "alg_ffn_get_timing", "alg_status_string", "alg_launch_count",
-    "alg_moe_create", "alg_moe_destroy", "alg_moe_workspace_bytes", "alg_moe_forward", "alg_moe_last_status",
+    "alg_moe_create", "alg_moe_destroy", "alg_moe_set_option", "alg_moe_workspace_bytes", "alg_moe_forward", "alg_moe_last_status",
     "alg_norm_create", "alg_norm_destroy", "alg_norm_set_option", "alg_norm_workspace_bytes", "alg_norm_forward", "alg_norm_backward", "alg_norm_last_status",
     "alg_ckpt_create", "alg_ckpt_destroy", "alg_ckpt_row_bytes", "alg_ckpt_store", "alg_ckpt_load", "alg_ckpt_act_forward",
     "alg_ckpt_act_backward",
@@ -103,6 +103,7 @@ def lib() -> ctypes.CDLL:
         L.alg_ffn_get_timing.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
         L.alg_moe_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, i32, i32, i32, ctypes.c_float, i32]
         L.alg_moe_destroy.argtypes = [vp]
+        L.alg_moe_set_option.argtypes = [vp, i32, i64]
         L.alg_moe_workspace_bytes.argtypes = [vp, i64, ctypes.POINTER(ctypes.c_size_t)]
         L.alg_moe_forward.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, vp, i64, i32, vp, vp, vp, ctypes.c_size_t, vp]
         L.alg_moe_last_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
@@ -463,6 +464,7 @@ class MoE(_Handle):
     """alg_moe_* : Y = sum_j weight_j * (silu(X W_gate[e_j]) .* (X W_up[e_j])) W_down[e_j], the experts e_j of a row chosen by
     its router scores.  W_router: D x E (``router_dtype``); W_gate_up: E x D x 2F, [W_gate | W_up]; W_down: E x F x D."""
     _destroy = "alg_moe_destroy"
+    _set_option = "alg_moe_set_option"
 
     def __init__(self, D, F, experts, top_k, score="softmax", renormalise=True, route_scale=1.0, router_dtype="bf16"):
         super().__init__()
@@ -474,9 +476,6 @@ class MoE(_Handle):
         self._device = torch.cuda.current_device()
         self._dev = torch.device("cuda", self._device)
         self._bytes = self.workspace_bytes(64)   # one size for every call: memory a captured call holds is never exchanged for more
-
-    def set_option(self, name, value):
-        raise NotImplementedError("mixture-of-experts handles have no options")
 
     def workspace_bytes(self, max_M: int) -> int:
         out = ctypes.c_size_t()

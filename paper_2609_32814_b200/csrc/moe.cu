@@ -44,6 +44,8 @@ struct alg_moe_s {
   int device = 0, num_sms = 148;
   int clusters = 0;           // of the first launch
   int *d_state = nullptr;     // status word, then the counters of both launches
+  long long wait_limit = kDefaultWaitLimit;
+  uint32_t stall = 0;
   size_t state_bytes = 0;
 };
 
@@ -85,6 +87,7 @@ struct MoeArgs {
   int *count;                 // [CTA]: arrivals at the unit whose first contributor it is
   int *status;
   long long wait_limit;
+  uint32_t stall;             // test aid: bytes that are expected of a chunk's rows beside their own, and never come
   int stages, stage_bytes;
   int off_sums, off_ring;     // sums by row; the ring; in front of them what `Chosen` and `Routes` point to
 };
@@ -297,7 +300,8 @@ __device__ void choose(const MoeArgs &a, const float *logits, uint8_t *scratch, 
   }
   consumer_barrier();
   if (warp >= rows) return;
-  const int mine = lane < a.k ? place[warp * a.k + lane] : -1;
+  int mine = lane < a.k ? place[warp * a.k + lane] : -1;
+  if (mine >= a.E) mine = -1;   // (only where the logits lie over copies that came too late: an index of nothing must not leave here)
   float w = mine >= 0 ? score(l[mine], top, sum) : 0.f;
   if (a.renormalise) {
     float s = w;
@@ -332,25 +336,38 @@ struct Ring {
   int s = 0;
   uint32_t parity = 0;
   bool failed = false;
+  __device__ __forceinline__ uint32_t gave_up() const { return full + 16 * kStages; }   // a word behind the barriers: some thread of the CTA did
+  __device__ __forceinline__ bool stopped() const {
+    uint32_t v;
+    asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(gave_up()) : "memory");
+    return v != 0;
+  }
   __device__ __forceinline__ uint32_t stage() const { return base + s * stage_bytes; }
   __device__ __forceinline__ void next() {
     if (++s == stages) s = 0, parity ^= 1;
   }
-  // After a wait that ran out nothing is right, but everybody still goes the same way to the end.
+  // A wait that runs out says so in the status word.  From then on nothing is right and nothing more is asked for, but everybody still goes the
+  // same way to the end, and whoever multiplies gives the copies on their way time to land before their memory is used for something else or handed on.
   __device__ __forceinline__ bool wait(uint32_t bar, uint32_t par, const MoeArgs &a) {
-    if (mbar_try_wait(bar, par)) return true;
     if (failed) return false;
+    if (mbar_try_wait(bar, par)) return true;
     const long long t0 = clock64();
     while (!mbar_try_wait(bar, par))
       if (clock64() - t0 > a.wait_limit) {
         failed = true;
+        asm volatile("st.volatile.shared.u32 [%0], 1;" ::"r"(gave_up()) : "memory");
         atomicExch(a.status, (int)ALG_ERR_DEVICE_TIMEOUT);
         return false;
       }
     return true;
   }
   __device__ __forceinline__ bool wait_full(const MoeArgs &a) { return wait(full + 8 * s, parity, a); }
-  __device__ __forceinline__ bool wait_empty(const MoeArgs &a) { return wait(empty + 8 * s, parity ^ 1, a); }
+  __device__ __forceinline__ bool wait_empty(const MoeArgs &a) { return wait(empty + 8 * s, parity ^ 1, a) && !stopped(); }
+  __device__ __forceinline__ void let_land() const {
+    if (failed)
+      for (const long long t0 = clock64(); clock64() - t0 < kLandCycles;) {
+      }
+  }
 };
 __device__ __forceinline__ Ring make_ring(const MoeArgs &a, uint8_t *smem, uint64_t *bars) {
   Ring r;
@@ -361,6 +378,7 @@ __device__ __forceinline__ Ring make_ring(const MoeArgs &a, uint8_t *smem, uint6
 }
 __device__ __forceinline__ void init_ring(uint64_t *bars, int stages) {   // one thread
   const uint32_t full = smem_u32(bars), empty = full + 8 * kStages;
+  bars[2 * kStages] = 0;
   for (int s = 0; s < stages; ++s) mbar_init(full + 8 * s, 2), mbar_init(empty + 8 * s, kWarps);   // two warps fetch, eight use
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
@@ -492,7 +510,7 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
               const __grid_constant__ CUtensorMap tm_d, const MoeArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ __align__(8) uint64_t bars[2 * kStages];
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 1];
   __shared__ int flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, P = a.M * a.k, most = most_chosen(P, a.E);
   const Chosen ch(smem, most, a.M);
@@ -521,7 +539,7 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
         if (!ring.wait_empty(a)) break;
         const uint32_t bar = ring.full + 8 * ring.s, st = ring.stage();
         if (warp > kWarps) {
-          mbar_expect_tx(bar, a.M * 128);
+          mbar_expect_tx(bar, a.M * 128 + a.stall);
           tma_load_2d(st + kChunk, &tm_x, bar, c * 64, 0);
         } else if (a.router_copies) {
           const int boxes = min(4, (a.E - mine.e0 + 63) / 64);
@@ -564,6 +582,7 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       if (lane == 0) mbar_arrive(ring.empty + 8 * ring.s);
       ring.next();
     }
+    ring.let_land();
     consumer_barrier();
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -611,7 +630,7 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
         if (!ring.wait_empty(a)) break;
         const uint32_t bar = ring.full + 8 * ring.s, st = ring.stage();
         if (warp > kWarps) {
-          mbar_expect_tx(bar, a.M * 128);
+          mbar_expect_tx(bar, a.M * 128 + a.stall);
           tma_load_2d(st + kChunk, &tm_x, bar, chunk * 64, 0);
         } else {
           mbar_expect_tx(bar, kChunk);
@@ -715,6 +734,7 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
     chunk = 0;
     if (++strip == strips) strip = 0, ++x;
   }
+  ring.let_land();
 }
 
 // ---- second launch -----------------------------------------------------------------------------------------------------
@@ -724,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_h, const MoeArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ __align__(8) uint64_t bars[2 * kStages];
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 1];
   __shared__ int flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, P = a.M * a.k, most = most_chosen(P, a.E);
   const Chosen ch(smem, most, a.M);
@@ -768,7 +788,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         const uint32_t bar = ring.full + 8 * ring.s, st = ring.stage();
         if (warp > kWarps) {
           const int p0 = ch.first[x], groups = (ch.first[x + 1] - p0 + 7) / 8;
-          mbar_expect_tx(bar, groups * group_bytes);
+          mbar_expect_tx(bar, groups * group_bytes + a.stall);
           for (int g = 0; g < groups; ++g) tma_load_4d(st + kChunk + g * group_bytes, &tm_h, bar, 0, p0 + g * 8, chunk * 2, 0);
         } else {
           mbar_expect_tx(bar, kChunk);
@@ -872,6 +892,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       }
     consumer_barrier();
   }
+  ring.let_land();
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
@@ -997,6 +1018,10 @@ alg_status_t alg_moe_destroy(alg_moe_t h) {
   return ALG_OK;
 }
 
+alg_status_t alg_moe_set_option(alg_moe_t h, alg_option_t option, int64_t value) {
+  return h ? wait_option(&h->wait_limit, &h->stall, option, value) : ALG_ERR_INVALID_ARG;
+}
+
 alg_status_t alg_moe_workspace_bytes(alg_moe_t h, int64_t max_M, size_t *bytes) {
   if (!h || !bytes || max_M < 0 || max_M > kMaxM) return ALG_ERR_INVALID_ARG;
   *bytes = moe_layout(*h, max_M).total;
@@ -1038,7 +1063,7 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   a.bias = select_bias, a.experts = experts, a.weights = weights;
   a.Y = Y, a.ldy = ldy;
   a.table = (int *)(ws + L.table), a.H = (__nv_bfloat16 *)(ws + L.h), a.ldh = hidden_pitch(h->F), a.part = (float4 *)(ws + L.part);
-  a.status = h->d_state, a.wait_limit = kDefaultWaitLimit;
+  a.status = h->d_state, a.wait_limit = h->wait_limit, a.stall = h->stall;
 
   const int tiles = row_tiles(M);
   CUtensorMap tm_up, tm_x, tm_down, tm_h;

@@ -63,3 +63,8 @@ def test_expert_handles_refuse_bad_arguments_first():
 def test_norm_handles_have_options():
     L = _lib()
     assert L.alg_norm_set_option(None, 5, 1000) == 1
+
+
+def test_expert_handles_have_options():
+    L = _lib()
+    assert L.alg_moe_set_option(None, 5, 1000) == 1

@@ -282,3 +282,26 @@ def test_empty_batch_and_refusals():
         with pytest.raises(binding.AlgError) as err:
             binding.MoE(d, f, e, k)
         assert err.value.code == code
+
+
+@pytest.mark.parametrize("m,d,f,e,k,router,out", [(1, 2048, 768, 128, 8, "bf16", torch.bfloat16), (40, 1024, 256, 33, 4, "f32", torch.float32),
+                                                  (64, 520, 200, 300, 6, "bf16", torch.bfloat16)])
+def test_a_wait_that_runs_out_ends_the_call(m, d, f, e, k, router, out):
+    """Rows that never come whole (their barriers are told to expect more bytes than are sent; every copy that is sent lands): the calls return, the status
+    word says so and reading it clears it and the handle's counters: the next call is right, bit for bit."""
+    layer = Layer(m, d, f, e, k, router=router)
+    first = layer.run(out_dtype=out)
+    layer.check(*first)
+    layer.h.set_option("test_stall_bytes", 1024)
+    for limit in (1000, 20000, 4_000_000):
+        layer.h.set_option("wait_limit_cycles", limit)
+        layer.run(out_dtype=out)
+        layer.run(out_dtype=out)
+        assert layer.h.last_status() == 6 and layer.h.last_status() == 0
+    layer.h.set_option("test_stall_bytes", 0)
+    layer.h.set_option("wait_limit_cycles", 4_000_000_000)
+    again = layer.run(out_dtype=out)
+    assert layer.h.last_status() == 0 and all(torch.equal(p, q) for p, q in zip(first, again))
+    for name, value in (("test_stall_bytes", 8), ("test_stall_bytes", 65552), ("wait_limit_cycles", 999), ("stage_k", 64)):
+        with pytest.raises(binding.AlgError):
+            layer.h.set_option(name, value)
