@@ -55,7 +55,8 @@ __global__ void __launch_bounds__(32 * kSlices) norm_sums_kernel(const SumsArgs 
   slice[y][0][x] = r;
   asm volatile("bar.sync 1, %0;" ::"n"(32 * kSums) : "memory");
   if (c >= a.D) return;
-  const float scale = a.alpha * (a.scale ? a.scale[c] : 1.f), w = a.alpha * (a.post_w ? a.post_w[c] : 1.f), b = a.alpha * (a.post_b ? a.post_b[c] : 0.f);
+  const auto times = [&](const float *v, float none) { return a.ctas ? a.alpha * (v ? v[c] : none) : 0.f; };   // (no rows: 0, whatever the vectors hold)
+  const float scale = times(a.scale, 1.f), w = times(a.post_w, 1.f), b = times(a.post_b, 0.f);
   if (y == 0 && a.d_pre_w) a.d_pre_w[c] = r;
   if (y == 1 && a.d_pre_b) a.d_pre_b[c] = r;
   if (y == 2 && a.d_post_w) a.d_post_w[c] = scale * r;

@@ -471,3 +471,16 @@ def test_a_wait_that_runs_out_ends_the_call(kind, dtype, stream, m, d, pitch):
         b.h.set_option("wait_limit_cycles", 999)
     with pytest.raises(binding.AlgError):
         b.h.set_option("stage_k", 64)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_sums_of_no_rows_are_zero_whatever_the_vectors_hold(kind):
+    b = Border(1, 64, kind, True, True, None, False, True, "bf16", "bf16")
+    e = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (math.inf, math.nan):
+        for k, v in b.vec.items():
+            v[::3] = bad
+        out = {k: torch.full((64,), 7.0, device="cuda") for k in b.vec}
+        got = b.h.backward(e, dY=e, dN=e, F=e, alpha=2.0, **b.vec, out=dict(out, R=e.clone()))
+        for k in b.vec:
+            assert bool((got[k] == 0).all()), k
