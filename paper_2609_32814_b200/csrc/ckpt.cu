@@ -7,7 +7,7 @@
 //
 // One pass over memory either way, eight columns (16 bytes of bf16) a thread: four neighbouring threads are a block and
 // find its maximum by two shuffles.  Bound by HBM: 16384 x 7168 fp32 stored and loaded 180 us (6.57 TB/s), SwiGLU 16384 x 6144 both
-// passes 290 us (6.28), GELU 8003 x 4096 71 us (5.54; with erff and one value an instruction 113, bound by the arithmetic), in fp32 115 (6.3).
+// passes 283 us (6.45), GELU 8003 x 4096 69 us (5.76; with erff and one value an instruction 113, bound by the arithmetic), in fp32 114 (6.3).
 #include <cuda_fp8.h>
 
 #include <new>
@@ -21,7 +21,7 @@ struct alg_ckpt_s {
   int cols = 0, parts = 1, padded = 0;   // columns of a part, parts, columns of a part as the records hold them
   alg_q8_t format = ALG_Q8_E4M3;
   alg_act_t act = ALG_ACT_NONE;
-  int device = 0, num_sms = 148;
+  int device = 0;
   int64_t row_bytes = 0;
 };
 
@@ -43,7 +43,7 @@ struct CkptArgs {
   int cols, padded, codes, scales;   // codes of a row; scales of a part
   int units;             // padded / 8: threads' pieces of a row
   uint32_t inv_units;    // ceil(2^32 / units)
-  int tile_rows;         // rows a CTA takes at a time
+  int tile_rows;         // rows of a CTA
   int int8;
 };
 
@@ -283,7 +283,7 @@ __device__ __forceinline__ F8 eight(const Raw8<T> &r) {
 // A thread's piece on its way: eight columns of a row (and the eight that go with them, of a gated matrix).
 template <typename T, int OP, bool GATED, bool VEC>
 struct Piece {
-  uint32_t r;     // row of the CTA's, whose first the pointers of `a` are at
+  uint32_t r;     // row
   int u;          // piece of the row
   bool on;
   Raw8<T> raw, raw2;
@@ -302,10 +302,11 @@ struct Piece {
     else put_any(v, turn, to, pitch, first, r, column(), a.cols);
   }
   // piece i of n; whole warps
-  __device__ __forceinline__ void ask(const CkptArgs &a, int i, int n, T *turn) {
+  __device__ __forceinline__ void ask(const CkptArgs &a, uint32_t row0, int i, int n, T *turn) {
     on = i < n;
     r = on ? __umulhi((uint32_t)i, a.inv_units) : 0u;
     u = on ? i - (int)r * a.units : 0;
+    r += row0;
     if (OP == kLoad || OP == kBackward) {
       w = w2 = make_uint2(0u, 0u), s = s2 = 0;
       if (on) {
@@ -373,23 +374,19 @@ struct Piece {
 // Two pieces of a thread are on their way at a time; one of a gated matrix, whose registers are better spent on threads (two: 312 us against
 // 300 at 16384 x 6144).  Small CTAs, as many as there are tiles: 512 threads 331 us, 256 302, 128 295, forty registers or more alike.
 template <typename T, int OP, int ACT, bool GATED, bool VEC>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 12 : 9) ckpt_kernel(const CkptArgs args) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 12 : 9) ckpt_kernel(const CkptArgs a) {
   __shared__ __align__(32) T turns[VEC ? 1 : kThreads / 32][VEC ? 1 : 256];
   T *const turn = turns[VEC ? 0 : threadIdx.x >> 5];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int64_t row0 = (int64_t)blockIdx.x * args.tile_rows; row0 < args.M; row0 += (int64_t)gridDim.x * args.tile_rows) {
-    const int n = (int)min((int64_t)args.tile_rows, args.M - row0) * args.units;   // (a multiple of four: a block is whole)
-    CkptArgs a = args;
-    a.in += row0 * args.pitch_in, a.out += row0 * args.pitch_out, a.again = args.again ? args.again + row0 * args.pitch_again : nullptr;
-    a.ckpt = args.ckpt ? args.ckpt + row0 * args.row_bytes : nullptr;
-    for (int i = threadIdx.x; i - (int)threadIdx.x < n; i += (GATED ? 1 : 2) * kThreads) {
-      Piece<T, OP, GATED, VEC> p, q;
-      p.ask(a, i, n, turn);
-      if (!GATED) q.ask(a, i + kThreads, n, turn);
-      p.template finish<ACT>(a, turn);
-      if (!GATED) q.template finish<ACT>(a, turn);
-    }
+  const uint32_t row0 = blockIdx.x * a.tile_rows;
+  const int n = (int)min((uint32_t)a.tile_rows, (uint32_t)a.M - row0) * a.units;   // (a multiple of four: a block is whole)
+  for (int i = threadIdx.x; i - (int)threadIdx.x < n; i += (GATED ? 1 : 2) * kThreads) {
+    Piece<T, OP, GATED, VEC> p, q;
+    p.ask(a, row0, i, n, turn);
+    if (!GATED) q.ask(a, row0, i + kThreads, n, turn);
+    p.template finish<ACT>(a, turn);
+    if (!GATED) q.template finish<ACT>(a, turn);
   }
 }
 
@@ -451,7 +448,7 @@ alg_status_t alg_ckpt_create(alg_ckpt_t *out, int cols, alg_q8_t format, alg_act
   h->cols = cols, h->parts = gated ? 2 : 1;
   h->padded = (cols + kBlock - 1) / kBlock * kBlock;
   h->format = format, h->act = act;
-  h->device = dev, h->num_sms = sms;
+  h->device = dev;
   h->row_bytes = ((int64_t)h->parts * (h->padded + h->padded / kBlock) + 31) / 32 * 32;
   *out = h;
   return ALG_OK;

@@ -69,8 +69,6 @@ constexpr int kLogitCols = 256;             // experts a CTA has logits of
 struct MoeArgs {
   int M, D, F, E, k, sigmoid, renormalise, y_f32, planes;
   float route_scale;
-  const __nv_bfloat16 *X;
-  int64_t ldx;
   const void *W_router;
   int router_f32, router_copies;   // copies: the router's rows lie on 16 bytes and are bf16
   const float *bias;
@@ -1058,7 +1056,6 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   a.M = (int)M, a.D = h->D, a.F = h->F, a.E = h->E, a.k = h->k;
   a.sigmoid = h->score == ALG_MOE_SIGMOID, a.renormalise = h->renormalise, a.route_scale = h->route_scale;
   a.y_f32 = y_dtype == ALG_F32, a.planes = a.y_f32 ? 3 : 2;
-  a.X = (const __nv_bfloat16 *)X, a.ldx = ldx;
   a.W_router = W_router, a.router_f32 = h->router_dtype == ALG_F32, a.router_copies = !a.router_f32 && on_16(W_router, h->E, er);
   a.bias = select_bias, a.experts = experts, a.weights = weights;
   a.Y = Y, a.ldy = ldy;

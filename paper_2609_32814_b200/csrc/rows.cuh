@@ -28,7 +28,6 @@ struct Raw8<__nv_bfloat16> {
     else a.x = v.x, a.y = v.y;
   }
   __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void set(int j, __nv_bfloat16 v) { ((__nv_bfloat16 *)&a)[j] = v; }
   __device__ __forceinline__ void get(float (&f)[8]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -41,7 +40,6 @@ struct Raw8<float> {
   __device__ __forceinline__ void load(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
   __device__ __forceinline__ void load4(int half, const float *p) { (half ? b : a) = *(const float4 *)p; }
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void set(int j, float v) { (j < 4 ? (float *)&a : (float *)&b)[j & 3] = v; }
   __device__ __forceinline__ void get(float (&f)[8]) const {
     f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
   }
