@@ -212,6 +212,14 @@ class _Handle:
             self._ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
         return self._ws
 
+    def _scratch(self, workspace, nbytes: int) -> torch.Tensor:
+        """The caller's workspace, packed memory on the handle's device, or the handle's own."""
+        if workspace is None:
+            return self._workspace(nbytes, self._dev)
+        if workspace.get_device() != self._device or not workspace.is_contiguous():
+            raise ValueError("the workspace must be packed memory on the handle's device")
+        return workspace
+
 
 def _keep_arg(table, custom_keep, q):
     if _TABLES[table] != ALG_TABLE_CUSTOM:
@@ -503,7 +511,7 @@ class MoE(_Handle):
             experts = torch.empty((M, self.top_k), dtype=torch.int32, device=self._dev) if experts is None else experts
             weights = torch.empty((M, self.top_k), dtype=torch.float32, device=self._dev) if weights is None else weights
         pairs = (M, self.top_k)
-        ws = workspace if workspace is not None else self._workspace(self._bytes, X.device)
+        ws = self._scratch(workspace, self._bytes)
         _check(lib().alg_moe_forward(self._h, X.data_ptr(), ldx, M, self._packed(W_router, "W_router", (self.D, self.E), self.router_type),
                                      None if select_bias is None else self._packed(select_bias, "select_bias", (self.E,), torch.float32),
                                      self._packed(W_gate_up, "W_gate_up", (self.E, self.D, 2 * self.F), torch.bfloat16),
@@ -632,7 +640,7 @@ class BlockNorm(_Handle):
         to = [own[k] if k in own else vec(got.get(k), "the gradient of " + k) for k in names]
         ws = None
         if to != [None] * 5:
-            ws = workspace if workspace is not None else self._workspace(self._bytes, Y.device)
+            ws = self._scratch(workspace, self._bytes)
         code = lib().alg_norm_backward(
             self._h, Y.data_ptr(), ldy, *rows(dY, "dY", M, st), *rows(dN, "dN", M, dt), *f_at, *g_at, *read[:3], alpha, read[3], M, *r_to, *f_to,
             *g_to, *to, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream))

@@ -305,3 +305,13 @@ def test_a_wait_that_runs_out_ends_the_call(m, d, f, e, k, router, out):
     for name, value in (("test_stall_bytes", 8), ("test_stall_bytes", 65552), ("wait_limit_cycles", 999), ("stage_k", 64)):
         with pytest.raises(binding.AlgError):
             layer.h.set_option(name, value)
+
+
+def test_a_workspace_that_the_gpu_cannot_reach_is_refused():
+    layer = Layer(4, 64, 64, 8, 2)
+    size = layer.h.workspace_bytes(4)
+    before = binding.launch_count()
+    for bad in (torch.empty(size, dtype=torch.uint8), torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            layer.run(workspace=bad)
+    assert binding.launch_count() == before

@@ -484,3 +484,14 @@ def test_sums_of_no_rows_are_zero_whatever_the_vectors_hold(kind):
         got = b.h.backward(e, dY=e, dN=e, F=e, alpha=2.0, **b.vec, out=dict(out, R=e.clone()))
         for k in b.vec:
             assert bool((got[k] == 0).all()), k
+
+
+def test_a_workspace_that_the_gpu_cannot_reach_is_refused():
+    b = Border(4, 64, "rms", True, True, None, False, True, "bf16", "bf16")
+    y, n = b.h.forward(b.R, **b.call())
+    size = b.h.workspace_bytes()
+    before = binding.launch_count()
+    for bad in (torch.empty(size, dtype=torch.uint8), torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            b.h.backward(y, dY=b.dY, dN=b.dN, **b.call(), workspace=bad)
+    assert binding.launch_count() == before
