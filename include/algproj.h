@@ -372,7 +372,7 @@ alg_status_t alg_proj_grad_last_status(alg_proj_grad_t h, void *stream, alg_stat
  * their sum if `renormalise` (a sum below 1e-20 counts as that), times route_scale:
  *     Y = sum_j weight_j * (silu(X W_gate[e_j]) .* (X W_up[e_j])) W_down[e_j]
  * W_gate_up: E banks [W_gate | W_up], each D x 2F packed; W_down: E banks F x D packed; all bf16.  Scores and sums are fp32; the
- * weighted hidden rows are held as two bf16 terms (16 significant bits) for a bf16 Y, as three (24) for an fp32 Y.
+ * weighted hidden rows are held as three bf16 terms, which have all bits of an fp32 value: a bf16 Y is an fp32 Y rounded once.
  * An expert whose select_bias is -infinity or NaN is never taken; a row that finds fewer than top_k experts has index -1 and weight 0
  * in the places left, and Y = 0 where it finds none.  A row with a logit that is infinite or NaN takes no expert: index -1, weight NaN, Y NaN.
  * `experts` (int32) and `weights` (fp32), both M x top_k packed, or NULL: the choice, best first.

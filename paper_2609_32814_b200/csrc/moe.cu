@@ -63,11 +63,12 @@ constexpr int kCols = 128;                  // of a unit (up: of the hidden stat
 constexpr int kUpPitch = 2 * kCols + 4, kDownPitch = kCols + 4;   // floats of a row of sums in shared memory
 constexpr int kAhead = 6;                   // chunks of a share of the second launch that the first asks into L2 (5 tokens, wide: 12 141.1 us, 6 139.8)
 constexpr int kSmemLimit = 225 * 1024;
+constexpr int kPlanes = 3;                  // bf16 terms that hold a weighted hidden value: all 24 bits of it (two, found at run time, were no faster: 24 rows 52 us against 49)
 constexpr int kMaxM = ALG_MOE_MAX_M;
 constexpr int kLogitCols = 256;             // experts a CTA has logits of
 
 struct MoeArgs {
-  int M, D, F, E, k, sigmoid, renormalise, y_f32, planes;
+  int M, D, F, E, k, sigmoid, renormalise, y_f32;
   float route_scale;
   const void *W_router;
   int router_f32, router_copies;   // copies: the router's rows lie on 16 bytes and are bf16
@@ -77,7 +78,7 @@ struct MoeArgs {
   void *Y;
   int64_t ldy;
   int *table;                 // workspace: the chosen experts, as `Chosen` lies in shared memory
-  __nv_bfloat16 *H;           // workspace: weighted hidden rows, [planes][M * k][ldh]
+  __nv_bfloat16 *H;           // workspace: weighted hidden rows, [kPlanes][M * k][ldh]
   int ldh;                    // F to the next multiple of 64
   float4 *part;               // workspace: partial sums, [CTA][2][M][256] of the first launch, [..][128] of the second
   int down_ctas, down_blocks; // of the second launch
@@ -661,10 +662,12 @@ moe_up_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       const int col = strip * kCols + c;
       if (col >= a.ldh) return;   // (columns from F on come out as zero: their weights are)
       const float w = r.pair_w[first + row];
+      // (with expf and a rounded quotient results are as far off, 4.7e-7 to 5.1e-7 of their norm: what the tensor core's sums of 64 leave)
       auto hidden = [&](float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u * w; };
       float v[4] = {hidden(gate.x, up.x), hidden(gate.y, up.y), hidden(gate.z, up.z), hidden(gate.w, up.w)};
       __nv_bfloat16 *dst = a.H + (size_t)(first + row) * a.ldh + col;
-      for (int p = 0; p < a.planes; ++p) {
+#pragma unroll
+      for (int p = 0; p < kPlanes; ++p) {
         __nv_bfloat16 b[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -778,7 +781,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   int64_t unit = begin / per_unit;
   const int at = (int)(begin - unit * per_unit);
   int x = at / per_expert, chunk = at - x * per_expert;
-  const int group_bytes = a.planes * 2048;   // eight hidden rows: [plane][64 columns, 64 more][8]
+  constexpr int group_bytes = kPlanes * 2048;   // eight hidden rows: [plane][64 columns, 64 more][8]
   if (warp >= kWarps) {
     if (lane == 0)
       for (int64_t i = begin; i < end; ++i) {
@@ -833,7 +836,8 @@ moe_down_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
           for (int t = 0; t < N; ++t) {
             if (t * 8 >= rows) continue;
             float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-            for (int p = 0; p < a.planes; ++p) {
+#pragma unroll
+            for (int p = 0; p < kPlanes; ++p) {
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 const uint32_t at = hs + t * group_bytes + p * 2048 + h * 1024;
@@ -907,7 +911,7 @@ MoeLayout moe_layout(const alg_moe_s &h, int64_t M) {
   const size_t P = (size_t)M * h.k;
   size_t off = 0;
   L.table = off, off = up256(off + (size_t)Chosen::words(most_chosen((int)P, h.E), (int)M) * 4);
-  L.h = off, off = up256(off + 3 * P * hidden_pitch(h.F) * 2);
+  L.h = off, off = up256(off + kPlanes * P * hidden_pitch(h.F) * 2);
   L.part = off, off = up256(off + (size_t)h.num_sms * 2 * M * 2 * kCols * sizeof(float));
   L.total = off;
   return L;
@@ -1055,7 +1059,7 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   MoeArgs a = {};
   a.M = (int)M, a.D = h->D, a.F = h->F, a.E = h->E, a.k = h->k;
   a.sigmoid = h->score == ALG_MOE_SIGMOID, a.renormalise = h->renormalise, a.route_scale = h->route_scale;
-  a.y_f32 = y_dtype == ALG_F32, a.planes = a.y_f32 ? 3 : 2;
+  a.y_f32 = y_dtype == ALG_F32;
   a.W_router = W_router, a.router_f32 = h->router_dtype == ALG_F32, a.router_copies = !a.router_f32 && on_16(W_router, h->E, er);
   a.bias = select_bias, a.experts = experts, a.weights = weights;
   a.Y = Y, a.ldy = ldy;
@@ -1088,8 +1092,8 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   if (e != cudaSuccess) return ALG_ERR_CUDA;
   const uint64_t dx[2] = {D, (uint64_t)M}, sx[1] = {(uint64_t)ldx * 2};
   const uint32_t bx[2] = {64, (uint32_t)M};
-  const uint64_t dh[4] = {64, (uint64_t)P, H / 64, 3}, sh[3] = {2 * H, 128, 2 * P * H};   // {column of a block, pair, column block, plane}
-  const uint32_t bh[4] = {64, 8, 2, (uint32_t)a.planes};
+  const uint64_t dh[4] = {64, (uint64_t)P, H / 64, kPlanes}, sh[3] = {2 * H, 128, 2 * P * H};   // {column of a block, pair, column block, plane}
+  const uint32_t bh[4] = {64, 8, 2, kPlanes};
   if (make_map_nd(&tm_x, X, 2, dx, sx, bx, 128) != cudaSuccess || make_map_nd(&tm_h, a.H, 4, dh, sh, bh, 128) != cudaSuccess) return ALG_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   size_t smem = 0;
@@ -1105,7 +1109,7 @@ alg_status_t alg_moe_forward(alg_moe_t h, const void *X, int64_t ldx, int64_t M,
   a.count = h->d_state + 4;
   if (launch_moe(up_kernel(tiles), h->clusters * kCluster, kCluster, smem, st, tm_up, tm_x, tm_r, tm_down, a) != cudaSuccess) return ALG_ERR_CUDA;
   a.blocks = D % 64 == 0;
-  if (!fit_ring(a, false, (size_t)a.M * kDownPitch * sizeof(float), kChunk + a.planes * tiles * 2048, 0, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
+  if (!fit_ring(a, false, (size_t)a.M * kDownPitch * sizeof(float), kChunk + kPlanes * tiles * 2048, 0, &smem)) return ALG_ERR_UNSUPPORTED_SHAPE;
   a.count = h->d_state + 4 + h->num_sms;
   return launch_moe(down_kernel(tiles), h->num_sms, 1, smem, st, tm_down, tm_h, a) == cudaSuccess ? ALG_OK : ALG_ERR_CUDA;
 }

@@ -315,3 +315,12 @@ def test_a_workspace_that_the_gpu_cannot_reach_is_refused():
         with pytest.raises(ValueError):
             layer.run(workspace=bad)
     assert binding.launch_count() == before
+
+
+@pytest.mark.parametrize("m,d,f,e,k", [(1, 2048, 768, 128, 8), (9, 520, 136, 33, 3), (64, 256, 128, 8, 2), (5, 136, 1032, 40, 1)])
+def test_a_bf16_result_is_the_fp32_result_rounded_once(m, d, f, e, k):
+    """Nothing on the way is held in fewer bits for a result of fewer."""
+    layer = Layer(m, d, f, e, k)
+    y, experts, weights = layer.run(out_dtype=torch.float32)
+    short = layer.run(out_dtype=torch.bfloat16)
+    assert torch.equal(short[0], y.bfloat16()) and torch.equal(short[1], experts) and torch.equal(short[2], weights)
