@@ -101,7 +101,8 @@ typedef enum {
 #define ALG_MAX_Q 32        /* general interaction tables (32-bit keep masks) */
 #define ALG_MAX_Q_LARGE 256 /* complete-graph law Q_q with equal group widths: the large-algebra path */
 
-/* Per-handle options (alg_proj_set_option / alg_ffn_set_option).  They replace process-wide
+/* Per-handle options (alg_proj_set_option / alg_ffn_set_option; the last two of this list also alg_norm_set_option and
+ * alg_moe_set_option).  They replace process-wide
  * switches: nothing in the library reads the environment.  Set them between forward calls,
  * not concurrently with one; a value the handle's shape cannot honour is refused with
  * ALG_ERR_UNSUPPORTED_SHAPE and changes nothing.
@@ -368,8 +369,8 @@ alg_status_t alg_proj_grad_last_status(alg_proj_grad_t h, void *stream, alg_stat
 /* ---- mixture of experts on a few tokens (serving) ------------------------------------------------------
  * The gated FFN whose weights each row chooses itself: with logits L = X W_router (X: M x D bf16, W_router: D x E packed, of
  * router_dtype) and scores P = softmax(L) over the E experts (SOFTMAX) or sigmoid(L) (SIGMOID), a row takes the top_k experts
- * with the largest P + select_bias (E fp32 values or NULL; equal ones in ascending order of the expert), with weights P, divided by
- * their sum if `renormalise` (a sum below 1e-20 counts as that), times route_scale:
+ * with the largest P + select_bias (E fp32 values; NULL: in the order of L, which no rounding of P spoils; equal ones in ascending
+ * order of the expert), with weights P, divided by their sum if `renormalise` (a sum below 1e-20 counts as that), times route_scale:
  *     Y = sum_j weight_j * (silu(X W_gate[e_j]) .* (X W_up[e_j])) W_down[e_j]
  * W_gate_up: E banks [W_gate | W_up], each D x 2F packed; W_down: E banks F x D packed; all bf16.  Scores and sums are fp32; the
  * weighted hidden rows are held as three bf16 terms, which have all bits of an fp32 value: a bf16 Y is an fp32 Y rounded once.
@@ -377,11 +378,13 @@ alg_status_t alg_proj_grad_last_status(alg_proj_grad_t h, void *stream, alg_stat
  * in the places left, and Y = 0 where it finds none.  A row with a logit that is infinite or NaN takes no expert: index -1, weight NaN, Y NaN.
  * `experts` (int32) and `weights` (fp32), both M x top_k packed, or NULL: the choice, best first.
  * 1 <= M <= ALG_MOE_MAX_M; D and F multiples of 8; E <= ALG_MOE_MAX_EXPERTS, top_k <= ALG_MOE_MAX_TOP_K; X, Y and the weights on 16 bytes, ldx in
- * multiples of 8, ldy of 16 bytes.  M = 0 is a successful no-op.  Only the experts that some row takes are read.  Two launches, no host
- * synchronisation.  Calls on one handle must be ordered on the GPU (each launch's CTAs count in memory of the handle which of
- * them is the last of a tile); calls of different handles may overlap.  No CTA waits for another cluster's.  Nothing is read ahead
- * of the previous kernel's end.  Y may not overlap any operand.  Workspace: alg_moe_workspace_bytes(h, M), 256-byte aligned, no
- * initialisation needed. */
+ * multiples of 8, ldy of 16 bytes.  Fastest with a bf16 router of E in multiples of 8 on 16 bytes (others are laid out value by value:
+ * with 2048 features a call takes 65 to 80 us more in bf16, 240 in fp32), D and F in multiples of 64 (else 1.4 times as long) and
+ * up to eight rows an expert.  M = 0 is a successful no-op.  Only the experts that some row takes are read.  Two launches, no
+ * host synchronisation.  Calls on one handle must be ordered on the GPU (each launch's CTAs count in memory of the handle which of
+ * them is the last of a tile); calls of different handles may overlap.  No CTA waits for another cluster's.  Nothing is used of
+ * what lies in memory before the previous kernel's end (the router is asked into L2, where that kernel's stores go).  Y may not
+ * overlap any operand.  Workspace: alg_moe_workspace_bytes(h, M), 256-byte aligned, no initialisation needed. */
 typedef enum { ALG_MOE_SOFTMAX = 0, ALG_MOE_SIGMOID = 1 } alg_moe_score_t;
 #define ALG_MOE_MAX_M 64
 #define ALG_MOE_MAX_EXPERTS 512
@@ -420,9 +423,10 @@ alg_status_t alg_moe_last_status(alg_moe_t h, void *stream, alg_status_t *status
  *              (which order depends on the types, the sizes and how the rows lie in their 16-byte words).
  * 1 <= D <= ALG_NORM_MAX_D.  Leading dimensions (below 2^30) and addresses may be anything an element may have.  Rows on 16 bytes run
  * fastest; rows that lie off it, but in all matrices alike, take up to twice as long; rows that lie each in its own way, and rows off 16
- * bytes of more than 8185 columns, several times.  Row b of an output may lie exactly on row b of an operand (Y on R, dR on
- * dY, ...: same address, leading dimension and row length in bytes); any other overlap is ALG_ERR_INVALID_ARG.  M = 0: forward
- * is a no-op, backward writes zero sums.  Workspace (backward): alg_norm_workspace_bytes, 256-byte aligned, no
+ * bytes of more than 8185 columns, several times.  In the backward pass fp32 F, dY == NULL, gradients that are not wanted, biases'
+ * gradients with RMS, and LayerNorm past 4096 columns take 1.7 to 4.5 times their bytes.  Row b of an output may lie exactly on row
+ * b of an operand (Y on R, dR on dY, ...: same address, leading dimension and row length in bytes); any other overlap is
+ * ALG_ERR_INVALID_ARG.  M = 0: forward is a no-op, backward writes zero sums.  Workspace (backward): alg_norm_workspace_bytes, 256-byte aligned, no
  * initialisation needed; calls that share one must be ordered on the GPU, others may overlap on any streams.  Forward is one launch,
  * backward two (one without column sums). */
 typedef enum { ALG_NORM_RMS = 0, ALG_NORM_LAYER = 1 } alg_norm_kind_t;

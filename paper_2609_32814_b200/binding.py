@@ -497,7 +497,8 @@ class MoE(_Handle):
 
     def forward(self, X, W_router, W_gate_up, W_down, select_bias=None, out=None, out_dtype=None, routing=False, experts=None, weights=None,
                 workspace=None, stream=None):
-        """Y, or (Y, experts, weights) with ``routing``: the rows' experts (int32) and their weights (fp32), M x top_k."""
+        """Y, or (Y, experts, weights) with ``routing``: the rows' experts (int32) and their weights (fp32), M x top_k.  Calls of a handle,
+        captured ones too, must follow one another on the GPU."""
         M = X.shape[0]
         ldx = _rows(X, "X", M, self.D, torch.bfloat16, self._device)
         if M > 64:
@@ -603,7 +604,8 @@ class BlockNorm(_Handle):
     def backward(self, Y, dY=None, dN=None, F=None, gate=None, post_weight=None, post_bias=None, scale=None, alpha=1.0, pre_weight=None,
                  pre_bias=None, want=None, out=None, workspace=None, stream=None):
         """The gradients, by name: "R", "F", "gate" and those of the vectors given.  ``want``: the names to compute (R always is) instead of
-        all of these; ``out``: tensors to write some of them to."""
+        all of these; ``out``: tensors to write some of them to.  Without ``workspace`` (``workspace_bytes`` bytes) the calls of a handle share
+        one: calls on several streams, or graphs that are replayed at the same time, need one each."""
         M, D, dev, st, dt, vec = Y.shape[0], self.D, self._device, self.stream_type, self.type, self._vector
         ldy = _rows(Y, "Y", M, D, st, dev)
         got = dict(out) if out else {}
